@@ -16,6 +16,14 @@
  *                        on this GPU (eq. dp_grad_avg; Algorithm 1 sum and /N)
  *   gift_decode          inverse transform of the averaged gradient
  *
+ * and, on either side of it, what makes the gradient of a token table and what
+ * the averaged gradients are for:
+ *
+ *   gift_embedding       embedding lookup
+ *   gift_embedding_grad  its gradient for each rank (an input of gift_encode)
+ *   gift_grad_norm       global gradient norm and clip coefficient
+ *   gift_adamw_step      AdamW over many tensors, float32 or 8-bit moments
+ *
  * Notation: m = d_out (rows), n = d_in (columns), N data-parallel ranks, r the
  * transform rank, T tokens behind the factor statistics.
  *
@@ -99,7 +107,11 @@ typedef enum {
   GIFT_KERNEL_DECODE_PROJECT = 12, /* the inverse transform's projections     */
   GIFT_KERNEL_CHOL_TRANSFORM = 13, /* Cholesky-form transform products         */
   GIFT_KERNEL_MXFP4 = 14,        /* MXFP4 scale + pack (gift_encode_mxfp4)     */
-  GIFT_KERNEL_COUNT = 15
+  GIFT_KERNEL_EMBED = 15,        /* embedding lookup                          */
+  GIFT_KERNEL_EMBED_GRAD = 16,   /* embedding gradient (sort and sums)        */
+  GIFT_KERNEL_NORM = 17,         /* gradient norm                             */
+  GIFT_KERNEL_OPTIMIZER = 18,    /* AdamW step                                */
+  GIFT_KERNEL_COUNT = 19
 } gift_kernel;
 
 /* ABI version of the loaded library (GIFT_ABI_VERSION it was built with). */
@@ -381,6 +393,145 @@ gift_status gift_decode(gift_ctx *ctx, const gift_factor *f, const float *mean,
  * listed twice. */
 gift_status gift_decode_batch(gift_ctx *ctx, int32_t count, const gift_factor *const *factors,
                               const float *const *means, float *const *outs, int64_t m, int64_t n);
+
+/* ---------------------------------------------------------------------------
+ * The training step around the codec
+ *
+ * These calls hold nothing between calls and read no host memory after they
+ * return, so they may be captured into a HIP graph.  The two that need device
+ * scratch (gift_embedding_grad, gift_grad_norm) take it as an argument: NULL
+ * is the context's workspace, which is ordered by the context's stream and may
+ * be reallocated by a later call, and is refused while the stream is being
+ * captured (GIFT_EUNSUPPORTED); a captured call passes scratch of the caller's
+ * that lives as long as the graph and that no other work uses while the graph
+ * runs.  The device that the context is bound to must be current (GIFT_EINVAL).
+ * ------------------------------------------------------------------------- */
+
+/* Integer type of token ids. */
+typedef enum { GIFT_I32 = 0, GIFT_I64 = 1 } gift_index_type;
+
+/* Embedding lookup: out[t] = scale * table[tokens[t]], rounded to out's type
+ * (to nearest even).
+ *   table   [V, d] float32 or bfloat16;
+ *   tokens  [T] int32 or int64.  An id outside [0, V) (padding) gives a row of
+ *           zeros;
+ *   out     [T, d] float32 or bfloat16; must not overlap table or tokens.
+ * The scale is applied in float32.  T may be 0.  Any element alignment.
+ * Errors: GIFT_EINVAL (NULL, bad type, scale not finite), GIFT_ESHAPE (T < 0 or
+ * T >= 2^31, V not in [1, 2^31 - 2], d not in [1, 2^20]). */
+gift_status gift_embedding(gift_ctx *ctx, const void *table, gift_dtype table_dtype, int64_t V,
+                           int64_t d, const void *tokens, gift_index_type token_type, int64_t T,
+                           float scale, void *out, gift_dtype out_dtype);
+
+/* Gradient of the lookup, for each of N ranks:
+ *   grads[j][v] = scale * sum over t with tokens[j][t] = v of dout[j][t]
+ *   tokens  [N, T] int32 or int64; ids outside [0, V) count for nothing (their
+ *           rows of dout are not read);
+ *   dout    [N, T, d] float32 or bfloat16;
+ *   grads   [N, V, d] float32 out, the grads of gift_encode.  accumulate = 0:
+ *           every row is written, rows without a token with zeros;
+ *           accumulate != 0: added to what grads holds (a table tied to the
+ *           output layer), rows without a token are neither read nor written.
+ *           Must not overlap the inputs.
+ *   scratch NULL or 256-byte aligned device memory of at least
+ *           gift_embedding_grad_scratch(N, T, V, d) bytes, scratch_bytes of it.
+ * Positions are ordered by token (a stable sort), a row's terms are added in
+ * float32 in runs of neighbouring positions, the runs' sums in order: the same
+ * inputs give the same bits.  T may be 0.  Any element alignment of dout and
+ * grads.
+ * Errors: GIFT_EINVAL (NULL, bad type, scale not finite, scratch too small or
+ * misaligned), GIFT_ESHAPE (N not in [1, 65535], T < 0, N T >= 2^31, V not in
+ * [1, 2^31 - 2], d not in [1, 2^20], or more work than one launch takes),
+ * GIFT_EUNSUPPORTED (scratch NULL under capture). */
+gift_status gift_embedding_grad(gift_ctx *ctx, const void *tokens, gift_index_type token_type,
+                                const void *dout, gift_dtype dtype, int32_t N, int64_t T, int64_t V,
+                                int64_t d, float scale, int32_t accumulate, float *grads,
+                                void *scratch, uint64_t scratch_bytes);
+
+/* Scratch bytes of gift_embedding_grad; 0 for T <= 0 and for sizes that it
+ * refuses. */
+uint64_t gift_embedding_grad_scratch(int32_t N, int64_t T, int64_t V, int64_t d);
+
+/* Scratch bytes of gift_grad_norm. */
+#define GIFT_GRAD_NORM_SCRATCH_BYTES 16384
+
+/* Global norm of many gradients, and the coefficient that clips it:
+ *   out[0] = norm = sqrt(sum of all squares);
+ *   out[1] = min(1, max_norm / (norm + 1e-6)), NaN when the norm is not finite.
+ *   grads, numel  HOST arrays of count device pointers and element counts
+ *                 (an entry of 0 elements is skipped, its pointer may be NULL),
+ *                 all float32 or all bfloat16;
+ *   max_norm      > 0; infinity clips nothing;
+ *   out           [2] float32 (device);
+ *   scratch       NULL or 8-byte aligned device memory of at least
+ *                 GIFT_GRAD_NORM_SCRATCH_BYTES, scratch_bytes of it.
+ * Squares and sums are float64.  out + 1 is the grad_scale of gift_adamw_step.
+ * Errors: GIFT_EINVAL (NULL, bad type, max_norm not > 0, scratch too small or
+ * misaligned, a gradient not aligned to its element), GIFT_ESHAPE (count < 0, an
+ * element count outside [0, 2^34]), GIFT_EUNSUPPORTED (scratch NULL under
+ * capture). */
+gift_status gift_grad_norm(gift_ctx *ctx, int32_t count, const void *const *grads,
+                           const int64_t *numel, gift_dtype dtype, double max_norm, float *out,
+                           void *scratch, uint64_t scratch_bytes);
+
+/* How gift_adamw_step keeps the moments. */
+typedef enum {
+  GIFT_MOMENTS_F32 = 0,   /* float32                                                    */
+  GIFT_MOMENTS_FP8 = 1    /* E4M3 codes, one float32 scale per 256 consecutive elements */
+} gift_moments;
+
+/* One tensor of gift_adamw_step (device pointers). */
+typedef struct {
+  float *param;           /* [numel] float32, updated                                   */
+  const void *grad;       /* [numel] float32 or bfloat16                                */
+  void *m, *v;            /* [numel] moments, updated: float32, or uint8 E4M3 codes     */
+  float *m_scales;        /* [ceil(numel / 256)] (GIFT_MOMENTS_FP8; else ignored)       */
+  float *v_scales;
+  void *copy;             /* NULL, or [numel] bfloat16: the new param, to nearest even  */
+  int64_t numel;          /* 0: skipped                                                 */
+  double weight_decay;
+} gift_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;           /* number of this step, from 1                                */
+  uint64_t seed;          /* of the 8-bit moments' rounding                             */
+  gift_dtype grad_dtype;
+  gift_moments moments;
+  const float *lr_dev;        /* NULL, or the learning rate on the device (before lr)   */
+  const int64_t *step_dev;    /* NULL, or the step on the device (before step): not     */
+                              /* written; a captured step advances it by itself         */
+  const float *grad_scale;    /* NULL, or a factor of every gradient on the device; NaN */
+                              /* skips the step: nothing is written                     */
+} gift_adamw_options;
+
+/* One AdamW step over count tensors (a HOST array), t the step's number:
+ *   g' = grad_scale * g
+ *   m  = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in float32, one rounding per operation.  The moments start as zeros (codes
+ * and scales 0).
+ * GIFT_MOMENTS_FP8: m and v of a step are computed from the stored values
+ * (code value * scale) and used for p before they are rounded.  Each block of
+ * 256 consecutive elements of a tensor gets the scale s = fl32(amax / 448) and
+ * y = fl32(x * fl32(448 / amax)) as in gift_encode, and y is rounded
+ * stochastically on E4M3's grid: with a 16-bit number r, up where the part
+ * beyond the lower grid point plus (r + 1/2) 2^-16 grid steps reaches a step.
+ * (To nearest, v would stand still: half a grid step is 3 to 6 % of a value.)
+ * A positive v is stored as at least the smallest positive code.  r of element
+ * e: u = e mod 512, word 2 (u / 256) + (u mod 4) / 2 of Philox4x32-10 with
+ * key = seed, counter (call lo, call hi, the tensor's index in the list, t mod
+ * 2^32), call = 64 (e / 512) + (u mod 256) / 4; its low half for even e, else
+ * its high half.  A NaN or an infinity in a block makes the block's moments NaN
+ * or 0, as in gift_encode.
+ * Tensors must not overlap each other.  param, grad and the scales 4-byte
+ * (bfloat16: 2-byte) aligned; float32 moments 4-byte aligned; codes any.
+ * Errors: GIFT_EINVAL (NULL, bad type, misaligned; lr or a weight decay not
+ * finite or negative, a beta outside [0, 1), eps not a positive float32 or not
+ * finite, step < 1 without step_dev), GIFT_ESHAPE (count < 0, numel outside
+ * [0, 2^34]). */
+gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *tensors,
+                            const gift_adamw_options *options);
 
 #ifdef __cplusplus
 }

@@ -14,6 +14,8 @@ Modules
 ``codec``     factor statistics, the low-rank transform, scaling, quantization,
               the local rank sum, the inverse transform and the reconstruction
               metrics (Sec. II-B, IV-A, V-A, V-B, Algorithm 1).
+``train``     the training step around the codec: embedding lookup and gradient,
+              gradient norm, AdamW with float32 and 8-bit moments.
 ``subspace``  the iterative rank-r eigen-step the GPU uses for the factor
               refresh, mirrored in float64, and the counter-based random
               generator that seeds it.
@@ -23,4 +25,4 @@ invariants, brute force on tiny inputs or library routines; see the pins listed
 in each function's docstring.
 """
 
-from . import e4m3, codec, subspace  # noqa: F401
+from . import e4m3, codec, subspace, train  # noqa: F401

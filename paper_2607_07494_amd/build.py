@@ -26,7 +26,7 @@ CALIB_SOURCE = "calib.hip"
 CALIB_LIB = os.path.join(PKG, "libgift_calib.so")
 
 SOURCES = ["gift_api.cpp", "k_tile.hip", "k_reduce.hip", "k_factor.hip", "k_small.hip", "k_syrk.hip", "k_update.hip", "k_stream.hip",
-           "k_lowrank.hip", "k_strip.hip", "k_chol.hip", "k_mx.hip"]
+           "k_lowrank.hip", "k_strip.hip", "k_chol.hip", "k_mx.hip", "gift_train.cpp", "k_embed.hip", "k_optim.hip"]
 
 
 def hipcc() -> str:

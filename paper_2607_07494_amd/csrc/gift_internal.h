@@ -410,4 +410,36 @@ gift_status grow_buffer(gift_ctx *ctx, Workspace &w, size_t bytes, void **out);
 gift_status upload_table(gift_ctx *ctx, int kind, const void *owner, const void *host, size_t bytes,
                          void **dev);
 
+// ---------------------------------------------------------------------------
+// The training step around the codec (k_embed.hip, k_optim.hip)
+// ---------------------------------------------------------------------------
+struct LookupJob {
+  const void *table = nullptr, *tokens = nullptr;
+  void *out = nullptr;
+  int64_t T = 0, V = 0, d = 0;
+  float scale = 1.f;
+  bool table_bf16 = false, out_bf16 = false, wide = false;   // wide: int64 ids
+};
+gift_status launch_lookup(gift_ctx *ctx, const LookupJob &job);
+
+struct EmbGradJob {
+  const void *tokens = nullptr, *dout = nullptr;
+  float *grads = nullptr;
+  int32_t N = 0;
+  int64_t T = 0, V = 0, d = 0;
+  float scale = 1.f;
+  bool bf16 = false, wide = false, accumulate = false;
+};
+size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d);
+// the waves of its largest launch; one launch takes up to kMaxWaves
+int64_t embgrad_waves(const EmbGradJob &job);
+constexpr int64_t kMaxWaves = (1LL << 26) - 4;   // 2^32 threads of a grid dimension
+gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &job, char *ws);
+
+size_t grad_norm_scratch();
+gift_status launch_grad_norm(gift_ctx *ctx, int32_t count, const void *const *grads, const int64_t *numel, bool bf16,
+                             double max_norm, float *out, double *part);
+gift_status launch_adamw(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *tensors,
+                         const gift_adamw_options &options);
+
 }  // namespace gift

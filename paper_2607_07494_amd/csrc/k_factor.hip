@@ -51,6 +51,7 @@
 
 #include "gift_internal.h"
 #include "k_small.h"
+#include "philox.h"
 
 namespace gift {
 
@@ -75,27 +76,6 @@ struct Member {
   float damping;
 };
 
-__device__ __forceinline__ uint32_t philox_word0(uint32_t c0, uint32_t c1, uint32_t c2,
-                                                 uint32_t c3, uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    if (r) {
-      k0 += 0x9E3779B9u;
-      k1 += 0xBB67AE85u;
-    }
-    const uint64_t p0 = (uint64_t)0xD2511F53u * c0;
-    const uint64_t p1 = (uint64_t)0xCD9E8D57u * c2;
-    const uint32_t hi0 = (uint32_t)(p0 >> 32), lo0 = (uint32_t)p0;
-    const uint32_t hi1 = (uint32_t)(p1 >> 32), lo1 = (uint32_t)p1;
-    const uint32_t n0 = hi1 ^ c1 ^ k0, n2 = hi0 ^ c3 ^ k1;
-    c0 = n0;
-    c1 = lo1;
-    c2 = n2;
-    c3 = lo0;
-  }
-  return c0;
-}
-
 // start rows of every member: warm rows from the member's Qt, the others from
 // the start block (grid.y = member)
 __global__ void gather_start_kernel(const Member *mem) {
@@ -110,7 +90,7 @@ __global__ void gather_start_kernel(const Member *mem) {
     if (warm) {
       v = M.Qt[t];
     } else {
-      const uint32_t w = philox_word0((uint32_t)i, (uint32_t)j, 0u, 0u, M.seed_lo, M.seed_hi);
+      const uint32_t w = philox((uint32_t)i, (uint32_t)j, 0u, 0u, M.seed_lo, M.seed_hi).w[0];
       v = (float)(((int32_t)w) >> 8) * 1.1920928955078125e-7f;
     }
     M.start[t] = v;

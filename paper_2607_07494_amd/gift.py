@@ -28,7 +28,10 @@ KERNELS = {
     "amax": 0, "quant": 1, "project": 2, "update_amax": 3, "update_quant": 4,
     "update_store": 5, "reduce": 6, "syrk": 7, "factor": 8, "small": 9,
     "chol": 10, "eig": 11, "decode_project": 12, "chol_transform": 13, "mxfp4": 14,
+    "embed": 15, "embed_grad": 16, "norm": 17, "optimizer": 18,
 }
+I32, I64 = 0, 1
+MOMENTS = {"f32": 0, "e4m3": 1}
 
 _STATUS = {OK: "GIFT_OK", EINVAL: "GIFT_EINVAL", ESHAPE: "GIFT_ESHAPE", ENOMEM: "GIFT_ENOMEM",
            EHIP: "GIFT_EHIP", EUNSUPPORTED: "GIFT_EUNSUPPORTED"}
@@ -38,6 +41,21 @@ class GiftError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{_STATUS.get(status, status)}: {message}")
         self.status = status
+
+
+class _AdamWTensor(ctypes.Structure):
+    """``gift_adamw_tensor``."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("numel", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
+class _AdamWOptions(ctypes.Structure):
+    """``gift_adamw_options``."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("grad_dtype", ctypes.c_int32), ("moments", ctypes.c_int32), ("lr_dev", ctypes.c_void_p),
+                ("step_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
 def _load():
@@ -80,6 +98,11 @@ def _load():
         "gift_reduce_local_mxfp4": ([P, P, P, I32, I64, I64, P], I32),
         "gift_decode": ([P, P, P, I64, I64, P], I32),
         "gift_decode_batch": ([P, I32, P, P, P, I64, I64], I32),
+        "gift_embedding": ([P, P, I32, I64, I64, P, I32, I64, F, P, I32], I32),
+        "gift_embedding_grad_scratch": ([I32, I64, I64, I64], U64),
+        "gift_embedding_grad": ([P, P, I32, P, I32, I32, I64, I64, I64, F, I32, P, P, U64], I32),
+        "gift_grad_norm": ([P, I32, P, P, I32, ctypes.c_double, P, P, U64], I32),
+        "gift_adamw_step": ([P, I32, ctypes.POINTER(_AdamWTensor), ctypes.POINTER(_AdamWOptions)], I32),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -512,3 +535,250 @@ def decode_batch(ctx: Context, factors, means, outs):
     ma = arr(*[_ptr(t, torch.float32, "means").value for t in means])
     oa = arr(*[_ptr(t, torch.float32, "outs").value for t in outs])
     _check(LIB.gift_decode_batch(ctx.handle, count, fa, ma, oa, m, n))
+
+
+# ---------------------------------------------------------------------------
+# The training step around the codec
+# ---------------------------------------------------------------------------
+
+def _value_dtype(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+
+
+def _index_type(t, name):
+    import torch
+    if t.dtype == torch.int32:
+        return I32
+    if t.dtype == torch.int64:
+        return I64
+    raise TypeError(f"{name} must be int32 or int64, not {t.dtype}")
+
+
+def _on_current_device(**tensors):
+    """Raise ValueError unless every tensor is contiguous and on the current device."""
+    import torch
+    for name, t in tensors.items():
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, not on the current device")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _scratch(t):
+    """``(pointer, bytes)`` of a scratch tensor, or of none."""
+    if t is None:
+        return None, 0
+    _on_current_device(scratch=t)
+    return ctypes.c_void_p(t.data_ptr()), t.numel() * t.element_size()
+
+
+def embedding(ctx: Context, table, tokens, out, scale: float = 1.0):
+    """``gift_embedding``: ``out[...] = scale * table[tokens[...]]``; table [V, d] and out
+    [*tokens.shape, d] float32 or bfloat16, tokens int32 or int64 (ids outside [0, V): zeros)."""
+    V, d = _dims(table, 2, "table")
+    _expect(out, tuple(tokens.shape) + (d,), "out")
+    td, it, od = _value_dtype(table, "table"), _index_type(tokens, "tokens"), _value_dtype(out, "out")
+    _on_current_device(table=table, tokens=tokens, out=out)
+    _check(LIB.gift_embedding(ctx.handle, table.data_ptr(), td, V, d, tokens.data_ptr(), it, tokens.numel(), scale,
+                              out.data_ptr(), od))
+
+
+def embedding_grad_scratch(N: int, T: int, V: int, d: int) -> int:
+    """Scratch bytes of :func:`embedding_grad` (``gift_embedding_grad_scratch``)."""
+    return LIB.gift_embedding_grad_scratch(N, T, V, d)
+
+
+def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumulate: bool = False, scratch=None):
+    """``gift_embedding_grad``: tokens [N, T], dout [N, T, d] (float32 or bfloat16) ->
+    grads [N, V, d] float32, each rank's gradient of the lookup; with ``accumulate``
+    added to what grads holds.  ``scratch``: a tensor of at least
+    :func:`embedding_grad_scratch` bytes (needed under graph capture), else the
+    context's workspace."""
+    import torch
+    N, V, d = _dims(grads, 3, "grads")
+    T = _dims(tokens, 2, "tokens")[1]
+    _expect(tokens, (N, T), "tokens")
+    _expect(dout, (N, T, d), "dout")
+    it, dt = _index_type(tokens, "tokens"), _value_dtype(dout, "dout")
+    if grads.dtype != torch.float32:
+        raise TypeError(f"grads must have dtype torch.float32, not {grads.dtype}")
+    _on_current_device(tokens=tokens, dout=dout, grads=grads)
+    ws, ws_bytes = _scratch(scratch)
+    _check(LIB.gift_embedding_grad(ctx.handle, tokens.data_ptr(), it, dout.data_ptr(), dt, N, T, V, d, scale,
+                                   1 if accumulate else 0, grads.data_ptr(), ws, ws_bytes))
+
+
+GRAD_NORM_SCRATCH_BYTES = 16384
+
+
+def _gradient_list(grads):
+    """``(dtype, data pointers)`` of a list of gradients on the current device, of one dtype."""
+    import torch
+    dev, dtype = torch.cuda.current_device(), grads[0].dtype
+    dt = _value_dtype(grads[0], "gradients")
+    ptrs = []
+    for g in grads:
+        if g.dtype != dtype:
+            raise TypeError(f"gradients must have one dtype: {g.dtype} and {dtype}")
+        if not g.is_cuda or g.device.index != dev:
+            raise ValueError(f"gradients must be on the current device, not on {g.device}")
+        if not g.is_contiguous():
+            raise ValueError("gradients must be contiguous")
+        ptrs.append(g.data_ptr())
+    return dt, ptrs
+
+
+def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=None):
+    """``gift_grad_norm``: out [2] float32 = the norm over all tensors of the list ``grads``
+    (all float32 or all bfloat16) and the coefficient that clips it to ``max_norm``
+    (NaN when the norm is not finite).  ``scratch``: a tensor of at least
+    ``GRAD_NORM_SCRATCH_BYTES`` bytes (needed under graph capture), else the
+    context's workspace."""
+    import torch
+    grads = list(grads)
+    _expect(out, (2,), "out")
+    if out.dtype != torch.float32:
+        raise TypeError(f"out must have dtype torch.float32, not {out.dtype}")
+    _on_current_device(out=out)
+    count = len(grads)
+    dt, ptrs = _gradient_list(grads) if count else (F32, [])
+    ws, ws_bytes = _scratch(scratch)
+    _check(LIB.gift_grad_norm(ctx.handle, count, (ctypes.c_void_p * count)(*ptrs),
+                              (ctypes.c_int64 * count)(*[g.numel() for g in grads]), dt, max_norm, out.data_ptr(),
+                              ws, ws_bytes))
+
+
+class AdamW:
+    """AdamW over a list of float32 tensors (``gift_adamw_step``).
+
+    ``moments``: ``"f32"``, or ``"e4m3"`` for FP8 E4M3 codes with a float32 scale
+    per 256 consecutive elements.  ``weight_decay``: one value, or one for each
+    tensor.  ``copies``: bfloat16 tensors of the parameters' shapes that every
+    step rewrites (entries may be ``None``).  ``state``: the moments, flat
+    tensors used in place (:meth:`state_sizes`); made as zeros when not given.
+    Tensor i's elements lie in ``m`` and ``v`` from ``starts[i]`` on (a multiple of
+    512), its scales in ``m_scales`` and ``v_scales`` from ``starts[i] // 256``.
+    """
+
+    ALIGN, BLOCK = 512, 256
+
+    def __init__(self, ctx: Context, params, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0,
+                 moments: str = "f32", seed: int = 0, state=None, copies=None):
+        import torch
+        if moments not in MOMENTS:
+            raise ValueError(f"moments must be one of {sorted(MOMENTS)}, not {moments!r}")
+        self.ctx, self.params, self.betas, self.eps, self.moments = ctx, list(params), betas, eps, moments
+        self.seed, self.steps = seed, 0
+        count = len(self.params)
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
+        self.copies = list(copies) if copies is not None else [None] * count
+        if len(decay) != count or len(self.copies) != count:
+            raise ValueError("weight_decay and copies must have one entry per parameter")
+        for p, c in zip(self.params, self.copies):
+            if p.dtype != torch.float32:
+                raise TypeError(f"parameters must be float32, not {p.dtype}")
+            if c is not None:
+                _expect(c, p.shape, "a copy")
+                if c.dtype != torch.bfloat16:
+                    raise TypeError(f"copies must be bfloat16, not {c.dtype}")
+        sizes = self.state_sizes(self.params, moments)
+        if state is not None:
+            if set(state) != set(sizes):
+                raise ValueError(f"state must hold {sorted(sizes)}, not {sorted(state)}")
+            for name, (n, dtype) in sizes.items():
+                _expect(state[name], (n,), f"state[{name!r}]")
+                if state[name].dtype != dtype:
+                    raise TypeError(f"state[{name!r}] must have dtype {dtype}, not {state[name].dtype}")
+        for p, c in zip(self.params, self.copies):
+            _on_current_device(parameter=p)
+            if c is not None:
+                _on_current_device(copy=c)
+        if state is None:
+            dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
+            state = {name: torch.zeros(n, dtype=dtype, device=dev) for name, (n, dtype) in sizes.items()}
+            if count:
+                # the zeros are written on torch's stream, the steps run on the context's
+                torch.cuda.current_stream().synchronize()
+        elif count:
+            _on_current_device(**state)
+        self.state = dict(state)
+        spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                 for t in self.params + [c for c in self.copies if c is not None] + list(self.state.values())]
+        spans = sorted(s for s in spans if s[1] > s[0])
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("parameters, copies and moments must not overlap")
+        self.starts = self._starts(self.params)[0]
+        self._tensors = (_AdamWTensor * count)()
+        for x, p, c, at, wd in zip(self._tensors, self.params, self.copies, self.starts, decay):
+            x.param, x.numel, x.weight_decay = p.data_ptr(), p.numel(), wd
+            x.copy = c.data_ptr() if c is not None else None
+            for name in ("m", "v"):
+                s = self.state[name]
+                setattr(x, name, s.data_ptr() + at * s.element_size())
+                if moments == "e4m3":
+                    setattr(x, name + "_scales", self.state[name + "_scales"].data_ptr() + at // self.BLOCK * 4)
+        self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
+                                      moments=MOMENTS[moments])
+
+    @classmethod
+    def _starts(cls, params):
+        starts, at = [], 0
+        for p in params:
+            starts.append(at)
+            at += -(-p.numel() // cls.ALIGN) * cls.ALIGN
+        return starts, at
+
+    @classmethod
+    def state_sizes(cls, params, moments: str = "f32"):
+        """``{name: (elements, dtype)}`` of the flat state tensors."""
+        import torch
+        total = cls._starts(params)[1]
+        if moments == "f32":
+            return {"m": (total, torch.float32), "v": (total, torch.float32)}
+        return {"m": (total, torch.uint8), "v": (total, torch.uint8),
+                "m_scales": (total // cls.BLOCK, torch.float32), "v_scales": (total // cls.BLOCK, torch.float32)}
+
+    def step(self, grads, lr, step=None, grad_scale=None):
+        """One step with ``grads`` (one per parameter, all float32 or all bfloat16).
+
+        ``lr``: a number, or a float32 tensor of one element.  ``step``: the step's
+        number from 1 (default: one more than the last one's), or an int64
+        tensor of one element, which the caller advances.  A captured step needs
+        both as tensors where they change from replay to replay.
+        ``grad_scale``: a float32 tensor of one element; NaN skips the step.
+        """
+        import torch
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("grads must have one entry per parameter")
+        for g, p in zip(grads, self.params):
+            if g.shape != p.shape:
+                raise ValueError(f"a gradient must have shape {tuple(p.shape)}, not {tuple(g.shape)}")
+        o = self._options
+        for name, x, dtype in (("lr", lr, torch.float32), ("step", step, torch.int64),
+                               ("grad_scale", grad_scale, torch.float32)):
+            if isinstance(x, torch.Tensor):
+                if x.dtype != dtype or x.numel() != 1:
+                    raise TypeError(f"{name} must be one {dtype} element")
+                _on_current_device(**{name: x})
+        if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
+            raise TypeError("grad_scale must be a tensor")
+        on_device = isinstance(step, torch.Tensor)
+        number = 0 if on_device else self.steps + 1 if step is None else int(step)
+        o.lr, o.lr_dev = (0.0, lr.data_ptr()) if isinstance(lr, torch.Tensor) else (lr, None)
+        o.step, o.step_dev = number, step.data_ptr() if on_device else None
+        o.grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
+        if grads:
+            o.grad_dtype, ptrs = _gradient_list(grads)
+            for x, ptr in zip(self._tensors, ptrs):
+                x.grad = ptr
+        _check(LIB.gift_adamw_step(self.ctx.handle, len(grads), self._tensors, ctypes.byref(o)))
+        if not on_device:
+            self.steps = number

@@ -1,0 +1,374 @@
+"""Gradient norm and AdamW step on an MI355X.
+
+The step's contract is one float32 rounding per operation, so moments, codes,
+scales, parameters and copies equal the oracle's float32 evaluation bit for
+bit.  Against the formula in float64 (one step from float32 moments):
+  m: two products and a sum, the gradient's factor and beta's own roundings: the
+     terms' magnitudes times 5 2^-24;
+  v: one more product: 7 2^-24 of v (all terms are positive);
+  p: the update is off by m's error over the denominator and at most
+     (7 / 2 + 7) 2^-24 of itself, and three roundings of p or of the update:
+     |error| <= 3 2^-24 |p| + 18 2^-24 lr / c1 (|b1 m| + |(1 - b1) g|) / denominator.
+The norm is a float64 sum rounded once: 2^-24, and 2^-23 is asked.
+"""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import e4m3, train
+
+pytestmark = pytest.mark.gpu
+
+gift = pytest.importorskip("paper_2607_07494_amd.gift")
+DEV = "cuda"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+F = np.float32
+LR, B1, B2, EPS = 3e-3, 0.9, 0.95, 1e-8
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    c = gift.Context()
+    yield c
+    torch.cuda.synchronize()
+    c.close()
+
+
+# ---------------------------------------------------------------------------
+# Norm
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[1], [0, 5, 0], [8191, 8192, 8193, 3], [7] * 300, [1_000_003, 64], [20_000_000, 1, 999]])
+def test_norm(ctx, sizes, dtype):
+    say("norm", sizes[:4], len(sizes), dtype)
+    gen = torch.Generator(device=DEV).manual_seed(len(sizes))
+    whole = [torch.randn(n + 3, generator=gen, device=DEV).to(DT[dtype]) for n in sizes]
+    grads = [w[k % 4:k % 4 + n] for k, (w, n) in enumerate(zip(whole, sizes))]      # every alignment
+    out = torch.empty(2, device=DEV)
+    gift.grad_norm(ctx, grads, out, max_norm=2.0)
+    torch.cuda.synchronize()
+    norm, coef = train.grad_norm([g.double().cpu().numpy() for g in grads], 2.0)
+    got = out.double().cpu().numpy()
+    assert abs(got[0] - norm) <= 2.0 ** -23 * norm and abs(got[1] - coef) <= 2.0 ** -23 * coef
+    first = out.clone()
+    gift.grad_norm(ctx, grads, out, max_norm=2.0)
+    torch.cuda.synchronize()
+    assert torch.equal(first, out)
+
+
+def test_norm_corners(ctx):
+    out = torch.empty(2, device=DEV)
+
+    def norm(grads, **kw):
+        gift.grad_norm(ctx, grads, out, **kw)
+        torch.cuda.synchronize()
+        return out.tolist()
+
+    x = torch.zeros(10, device=DEV)
+    assert norm([], max_norm=1.0) == [0.0, 1.0] and norm([x], max_norm=1.0) == [0.0, 1.0]
+    x[3], x[4] = 3e20, 4e20                    # squares past float32
+    a, b = norm([x], max_norm=1.0)
+    assert abs(a / 5e20 - 1) <= 2.0 ** -23 and abs(b / 2e-21 - 1) <= 2.0 ** -22
+    assert norm([x])[1] == 1.0                 # no limit
+    x[5] = float("inf")
+    a, b = norm([x], max_norm=1.0)
+    assert math.isinf(a) and math.isnan(b)
+    x[5] = float("nan")
+    a, b = norm([x])
+    assert math.isnan(a) and math.isnan(b)
+
+
+# ---------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------
+class Case:
+    """Tensors of odd sizes and alignments on the GPU beside their oracle state."""
+
+    def __init__(self, ctx, sizes, moments, dtype, seed=1, copies=True, offsets=(0, 1, 2, 3), **kw):
+        rng = np.random.default_rng(seed)
+        self.moments, self.dtype, self.seed, self.decay = moments, dtype, 77 + seed, [0.1 * (k % 3) for k in range(len(sizes))]
+        self.offsets = [offsets[k % len(offsets)] for k in range(len(sizes))]
+        self.p = [rng.standard_normal(n).astype(F) for n in sizes]
+        self.m = [np.zeros(n, F) for n in sizes]
+        self.v = [np.zeros(n, F) for n in sizes]
+        self.whole = [torch.full((n + o + 8,), 9.0, device=DEV) for n, o in zip(sizes, self.offsets)]
+        self.params = [w[o:o + n] for w, n, o in zip(self.whole, sizes, self.offsets)]
+        for t, p in zip(self.params, self.p):
+            t.copy_(torch.from_numpy(p))
+        self.copies = [torch.zeros(n + o, dtype=torch.bfloat16, device=DEV)[o:] if copies and k % 3 < 2 else None
+                       for k, (n, o) in enumerate(zip(sizes, self.offsets))]
+        self.opt = gift.AdamW(ctx, self.params, betas=(B1, B2), eps=EPS, weight_decay=self.decay, moments=moments,
+                              seed=self.seed, copies=self.copies, **kw)
+        if moments == "e4m3":
+            self.code = [[np.zeros(n, np.uint8), np.zeros(n, np.uint8)] for n in sizes]
+            self.scale = [[np.zeros(-(-n // 256), F), np.zeros(-(-n // 256), F)] for n in sizes]
+
+    def gradients(self, rng, spread=2.0):
+        out = []
+        for k, (p, o) in enumerate(zip(self.p, self.offsets)):
+            g = torch.zeros(p.size + o, dtype=DT[self.dtype])
+            g[o:] = torch.from_numpy((rng.standard_normal(p.size) * 10.0 ** rng.uniform(-spread, 0, p.size) * 1e-3).astype(F)).to(DT[self.dtype])
+            out.append(g.to(DEV)[o:])
+        return out
+
+    def oracle_step(self, grads, lr, step, scale=1.0):
+        for k, g in enumerate(grads):
+            g = g.float().cpu().numpy()
+            if self.moments == "e4m3":
+                self.m[k], self.v[k] = (train.decode_moment(c, s) for c, s in zip(self.code[k], self.scale[k]))
+            self.m[k], self.v[k] = train.adamw_moments(self.m[k], self.v[k], g, B1, B2, scale)
+            self.p[k] = train.adamw_param(self.p[k], self.m[k], self.v[k], lr, B1, B2, EPS, self.decay[k], step)
+            if self.moments == "e4m3":
+                r = train.random_numbers(g.size, k, step, self.seed)
+                for j, (x, keep) in enumerate(((self.m[k], False), (self.v[k], True))):
+                    self.code[k][j], self.scale[k][j] = train.stochastic_codes(x, r, keep)
+
+    def check(self):
+        torch.cuda.synchronize()
+        for k, (t, p, o, w) in enumerate(zip(self.params, self.p, self.offsets, self.whole)):
+            np.testing.assert_array_equal(t.cpu().numpy(), p, err_msg=f"parameter {k}")
+            assert bool((w[:o] == 9).all()) and bool((w[o + p.size:] == 9).all())
+            if self.copies[k] is not None:
+                got = self.copies[k].cpu().view(torch.int16).numpy().view(np.uint16)
+                np.testing.assert_array_equal(got, train.to_bf16(p), err_msg=f"copy {k}")
+            at = self.opt.starts[k]
+            for j, name in enumerate("mv"):
+                flat = self.opt.state[name][at:at + -(-p.size // 512) * 512].cpu().numpy()
+                if self.moments == "f32":
+                    np.testing.assert_array_equal(flat[:p.size], (self.m, self.v)[j][k], err_msg=f"{name} {k}")
+                else:
+                    np.testing.assert_array_equal(flat[:p.size], self.code[k][j], err_msg=f"{name} codes {k}")
+                    blocks = -(-p.size // 256)
+                    s = self.opt.state[name + "_scales"][at // 256:at // 256 + -(-p.size // 512) * 2].cpu().numpy()
+                    np.testing.assert_array_equal(s[:blocks], self.scale[k][j], err_msg=f"{name} scales {k}")
+                    assert not s[blocks:].any()
+                assert not flat[p.size:].any()                     # behind the tensor
+
+
+SIZES = [1, 3, 64, 255, 256, 257, 511, 512, 513, 0, 2047, 2048, 2049, 4095, 4096, 4097, 10_001, 33_000]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("moments", ["f32", "e4m3"])
+def test_steps_equal_the_oracle(ctx, moments, dtype):
+    c = Case(ctx, SIZES, moments, dtype)
+    rng = np.random.default_rng(5)
+    scale = torch.tensor([0.3], device=DEV)
+    for step in range(1, 5):
+        say("adamw", moments, dtype, "step", step)
+        grads = c.gradients(rng)
+        with_scale = step % 2 == 0
+        c.opt.step(grads, lr=LR * step, grad_scale=scale if with_scale else None)
+        c.oracle_step(grads, LR * step, step, 0.3 if with_scale else 1.0)
+        c.check()
+    assert c.opt.steps == 4
+
+
+@pytest.mark.parametrize("moments", ["f32", "e4m3"])
+def test_more_tensors_than_a_launch_takes(ctx, moments):
+    c = Case(ctx, [100 + k for k in range(150)], moments, "f32", seed=2)
+    rng = np.random.default_rng(6)
+    for step in (1, 2):
+        grads = c.gradients(rng)
+        c.opt.step(grads, lr=LR)
+        c.oracle_step(grads, LR, step)
+    c.check()
+
+
+@pytest.mark.parametrize("moments", ["f32", "e4m3"])
+def test_aligned_tensors_and_a_late_step(ctx, moments):
+    """Every element on the vector path but the tails; a step number past 2^32."""
+    c = Case(ctx, [4096 * 3, 8192 + 4, 512 * 5, 6000], moments, "bf16", seed=3, offsets=(0, 8))
+    rng = np.random.default_rng(7)
+    for step in (2 ** 33 + 5, 2 ** 33 + 6):
+        grads = c.gradients(rng)
+        c.opt.step(grads, lr=LR, step=step)
+        c.oracle_step(grads, LR, step)
+    c.check()
+
+
+def test_one_step_against_the_formula_in_64_bits(ctx):
+    n, step, lr, wd, s = 50_000, 7, 1e-2, 0.1, 0.5
+    rng = np.random.default_rng(8)
+    p, g = rng.standard_normal(n).astype(F), (rng.standard_normal(n) * 1e-3).astype(F)
+    m, v = (rng.standard_normal(n) * 3e-4).astype(F), (rng.standard_normal(n).astype(F) * F(1e-3)) ** 2
+    total = -(-n // 512) * 512
+    state = {k: torch.zeros(total, device=DEV) for k in "mv"}
+    for k, x in (("m", m), ("v", v)):
+        state[k][:n] = torch.from_numpy(x)
+    param = torch.from_numpy(p).to(DEV)
+    opt = gift.AdamW(ctx, [param], betas=(B1, B2), eps=EPS, weight_decay=wd, state=state)
+    opt.step([torch.from_numpy(g).to(DEV)], lr=lr, step=step, grad_scale=torch.tensor([s], device=DEV))
+    torch.cuda.synchronize()
+    wp, wm, wv = train.adamw_formula(p, m, v, g, lr, B1, B2, EPS, wd, step, s)
+    u = 2.0 ** -24
+    terms = np.abs(B1 * m.astype(float)) + np.abs((1 - B1) * s * g.astype(float))
+    assert np.all(np.abs(state["m"][:n].cpu().numpy() - wm) <= 5 * u * terms)
+    assert np.all(np.abs(state["v"][:n].cpu().numpy() - wv) <= 7 * u * wv)
+    denominator = np.sqrt(wv / (1 - B2 ** step)) + EPS
+    assert np.all(np.abs(param.cpu().numpy() - wp) <= 3 * u * np.abs(p) + 18 * u * lr / (1 - B1 ** step) * terms / denominator)
+
+
+def test_moments_of_8_bits_are_right_in_the_mean(ctx):
+    """m and v stored over 400 seeds: the mean of a stored value is the value, to 6 standard errors of a rounding whose
+    values are at most one grid step apart, a standard deviation of half a step: 6 * step / (2 sqrt(400)) = 0.15 steps."""
+    n, runs = 512, 400
+    rng = np.random.default_rng(9)
+    g = (rng.standard_normal(n) * 1e-3).astype(F)
+    grad, param = torch.from_numpy(g).to(DEV), torch.zeros(n, device=DEV)
+    sums = {k: np.zeros(n) for k in "mv"}
+    table = e4m3.decode_table()
+    for seed in range(runs):
+        opt = gift.AdamW(ctx, [param], betas=(B1, B2), eps=EPS, moments="e4m3", seed=seed)
+        opt.step([grad], lr=0.0)
+        torch.cuda.synchronize()
+        for k in "mv":
+            scale = np.repeat(opt.state[k + "_scales"].cpu().numpy().astype(float), 256)
+            sums[k] += table[opt.state[k].cpu().numpy()] * scale
+    m, v = train.adamw_moments(np.zeros(n, F), np.zeros(n, F), g, B1, B2)
+    for k, x in (("m", m), ("v", v)):
+        x = x.astype(float)
+        y = np.abs(x) / np.repeat(np.abs(x).reshape(2, 256).max(1), 256) * 448
+        step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(y, 1e-30))), -6) - 3) / 448 * np.repeat(np.abs(x).reshape(2, 256).max(1), 256)
+        above = y >= 2.0 ** -9 if k == "v" else np.ones(n, bool)      # a positive v keeps the smallest code
+        assert np.all((np.abs(sums[k] / runs - x) <= 0.15 * step)[above]), k
+
+
+def test_a_nan_factor_skips_the_step(ctx):
+    for moments in ("f32", "e4m3"):
+        c = Case(ctx, [1000, 4096], moments, "f32", seed=4)
+        rng = np.random.default_rng(10)
+        grads = c.gradients(rng)
+        c.opt.step(grads, lr=LR)
+        c.oracle_step(grads, LR, 1)
+        c.opt.step(grads, lr=LR, step=2, grad_scale=torch.full((1,), float("nan"), device=DEV))
+        c.check()
+
+
+def test_a_nan_gradient_stays_in_its_place(ctx):
+    """float32 moments: one element; 8-bit: the moments of its block."""
+    for moments in ("f32", "e4m3"):
+        p = torch.ones(1024, device=DEV)
+        g = torch.full((1024,), 1e-3, device=DEV)
+        g[300] = float("nan")
+        opt = gift.AdamW(ctx, [p], moments=moments)
+        opt.step([g], lr=LR)
+        torch.cuda.synchronize()
+        assert torch.isnan(p).nonzero().flatten().tolist() == [300]
+        if moments == "f32":
+            assert torch.isnan(opt.state["m"]).nonzero().flatten().tolist() == [300]
+        else:
+            nan = (opt.state["v"] & 127) == 127
+            assert bool(nan[256:512].all()) and int(nan.sum()) == 256
+            assert torch.isnan(opt.state["m_scales"]).tolist() == [False, True, False, False]
+
+
+def test_zero_tiny_and_infinite_gradients(ctx):
+    g = np.zeros(768, F)
+    g[256:512] = 1e-30                 # squares below float32's range: v = 0, the update is m / eps
+    g[512:] = 1e-3
+    g[600] = np.inf
+    for moments in ("f32", "e4m3"):
+        p = torch.ones(768, device=DEV)
+        opt = gift.AdamW(ctx, [p], betas=(B1, B2), eps=EPS, moments=moments, seed=3)
+        opt.step([torch.from_numpy(g).to(DEV)], lr=LR)
+        torch.cuda.synchronize()
+        m, v = train.adamw_moments(np.zeros(768, F), np.zeros(768, F), g, B1, B2)
+        np.testing.assert_array_equal(p.cpu().numpy(), train.adamw_param(np.ones(768, F), m, v, LR, B1, B2, EPS, 0.0, 1))
+        if moments == "e4m3":
+            r = train.random_numbers(768, 0, 1, 3)
+            for k, x, keep in (("m", m, False), ("v", v, True)):
+                codes, scales = train.stochastic_codes(x, r, keep)
+                np.testing.assert_array_equal(opt.state[k][:768].cpu().numpy(), codes)
+                np.testing.assert_array_equal(opt.state[k + "_scales"][:3].cpu().numpy(), scales)
+
+
+def test_captured_steps_advance_by_device_scalars(ctx):
+    """Norm, clip and step in one graph on another stream, replayed between eager work: the step's number and the
+    learning rate come from the device."""
+    s = torch.cuda.Stream()
+    other = gift.Context(stream=s.cuda_stream)
+    for moments in ("f32", "e4m3"):
+        c = Case(other, [700, 4096, 9000], moments, "f32", seed=5)
+        rng = np.random.default_rng(11)
+        grads = c.gradients(rng)
+        step = torch.zeros(1, dtype=torch.int64, device=DEV)
+        lr = torch.zeros(1, device=DEV)
+        out = torch.zeros(2, device=DEV)
+        scratch = torch.empty(gift.GRAD_NORM_SCRATCH_BYTES, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step.add_(1)
+            with pytest.raises(gift.GiftError, match="scratch"):
+                gift.grad_norm(other, grads, out)
+            gift.grad_norm(other, grads, out, max_norm=0.05, scratch=scratch)
+            c.opt.step(grads, lr=lr, step=step, grad_scale=out[1:])
+        for k in range(1, 5):
+            fresh = c.gradients(rng)
+            for g, x in zip(grads, fresh):
+                g.copy_(x)
+            lr.fill_(LR * k)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            norm, coef = train.grad_norm([g.double().cpu().numpy() for g in grads], 0.05)
+            got = out.cpu().numpy()
+            assert abs(got[0] - norm) <= 2.0 ** -23 * norm and abs(got[1] - coef) <= 2.0 ** -23 * coef
+            c.oracle_step(grads, float(F(LR * k)), k, got[1])
+            c.check()
+    other.close()
+
+
+def test_state_tensors_are_used_in_place_and_overlap_is_refused(ctx):
+    p = torch.zeros(600, device=DEV)
+    sizes = gift.AdamW.state_sizes([p], "e4m3")
+    state = {k: torch.zeros(n, dtype=t, device=DEV) for k, (n, t) in sizes.items()}
+    opt = gift.AdamW(ctx, [p], moments="e4m3", state=state)
+    opt.step([torch.ones(600, device=DEV)], lr=LR)
+    torch.cuda.synchronize()
+    assert bool(state["m"][:600].all()) and not bool(state["m"][600:].any())
+    with pytest.raises(ValueError, match="overlap"):
+        gift.AdamW(ctx, [p, p])
+    with pytest.raises(ValueError, match="overlap"):
+        gift.AdamW(ctx, [p[:300], p[299:]])
+    with pytest.raises(ValueError, match="contiguous"):
+        gift.AdamW(ctx, [torch.zeros((4, 6), device=DEV).t()])
+    with pytest.raises(ValueError, match="contiguous"):
+        gift.AdamW(ctx, [torch.zeros((6, 4), device=DEV)]).step([torch.zeros((4, 6), device=DEV).t()], lr=LR)
+    with pytest.raises(TypeError, match="one dtype"):
+        gift.grad_norm(ctx, [p, p.bfloat16()], torch.empty(2, device=DEV))
+
+
+def test_elements_past_32_bits(ctx):
+    """A tensor of more than 2^32 bytes and 2^31 elements, 8-bit moments: its last elements against the oracle."""
+    n = 2 ** 31 + 700
+    p, g = torch.full((n,), 0.5, device=DEV), torch.full((n,), 1e-3, dtype=torch.bfloat16, device=DEV)
+    opt = gift.AdamW(ctx, [p], betas=(B1, B2), eps=EPS, moments="e4m3", seed=12)
+    opt.step([g], lr=LR)
+    torch.cuda.synchronize()
+    tail = 1024 + 700                # from a multiple of 512 on
+    gt = g[-tail:].float().cpu().numpy()
+    m, v = train.adamw_moments(np.zeros(tail, F), np.zeros(tail, F), gt, B1, B2)
+    np.testing.assert_array_equal(p[-tail:].cpu().numpy(), train.adamw_param(np.full(tail, 0.5, F), m, v, LR, B1, B2, EPS, 0.0, 1))
+    assert bool((p == p[-1]).all())
+    # the numbers of a group far in: the call's counter is 64 * (group) + lane, past 2^28
+    from oracle.subspace import philox4x32_10
+    e = np.arange(n - tail, n, dtype=np.int64)
+    u = e % 512
+    call = (e // 512) * 64 + (u % 256) // 4
+    w = np.stack(philox4x32_10(call & 0xFFFFFFFF, call >> 32, np.zeros(tail, np.int64), np.ones(tail, np.int64), 12, 0))
+    word = w[2 * (u // 256) + (u % 4) // 2, np.arange(tail)].astype(np.uint32)
+    r = np.where(e % 2 == 0, word & 0xFFFF, word >> 16).astype(np.int64)
+    codes, scales = train.stochastic_codes(v, r, True)
+    np.testing.assert_array_equal(opt.state["v"][n - tail:n].cpu().numpy(), codes)
+    np.testing.assert_array_equal(opt.state["v_scales"][(n - tail) // 256:-(-n // 256)].cpu().numpy(), scales)
