@@ -509,26 +509,31 @@ typedef struct {
  *   g' = grad_scale * g
  *   m  = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
  *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in float32, one rounding per operation.  The moments start as zeros (codes
- * and scales 0).
- * GIFT_MOMENTS_FP8: m and v of a step are computed from the stored values
- * (code value * scale) and used for p before they are rounded.  Each block of
- * 256 consecutive elements of a tensor gets the scale s = fl32(amax / 448) and
- * y = fl32(x * fl32(448 / amax)) as in gift_encode, and y is rounded
+ * The moments start as zeros (codes and scales 0).
+ * Every operation is float32 with one rounding, in this order; 1 - beta,
+ * 1 - lr weight_decay, lr / (1 - beta1^t) and 1 / sqrt(1 - beta2^t) are formed
+ * in float64 and rounded once.
+ * GIFT_MOMENTS_FP8: the old m and v are code value * scale.  p's update has a
+ * square root and a reciprocal of 1 ulp each (a v below 2^-126 may count as 0).
+ * The new m and v, once used for p, are stored: each block of 256 consecutive
+ * elements of a tensor as codes of y = x * (448 * (1 / amax)) (a multiplier of 0
+ * for amax = 0, at most FLT_MAX) with the scale amax * (1 / 448).  y is rounded
  * stochastically on E4M3's grid: with a 16-bit number r, up where the part
- * beyond the lower grid point plus (r + 1/2) 2^-16 grid steps reaches a step.
+ * beyond the lower grid point plus (r + 1/2) 2^-16 grid steps reaches a step
+ * (below 2^-6, fl32(y + 2^-6) - 2^-6 stands for y).
  * (To nearest, v would stand still: half a grid step is 3 to 6 % of a value.)
- * A positive v is stored as at least the smallest positive code.  r of element
+ * A v whose y is positive is stored as at least the smallest positive code.  r of element
  * e: u = e mod 512, word 2 (u / 256) + (u mod 4) / 2 of Philox4x32-10 with
  * key = seed, counter (call lo, call hi, the tensor's index in the list, t mod
  * 2^32), call = 64 (e / 512) + (u mod 256) / 4; its low half for even e, else
- * its high half.  A NaN or an infinity in a block makes the block's moments NaN
- * or 0, as in gift_encode.
+ * its high half.  A block with a NaN gets NaN codes; one with an infinity gets
+ * an infinite scale, a NaN code there and zeros elsewhere: either way its
+ * moments are NaN from then on.
  * Tensors must not overlap each other.  param, grad and the scales 4-byte
  * (bfloat16: 2-byte) aligned; float32 moments 4-byte aligned; codes any.
  * Errors: GIFT_EINVAL (NULL, bad type, misaligned; lr or a weight decay not
- * finite or negative, a beta outside [0, 1), eps not a positive float32 or not
- * finite, step < 1 without step_dev), GIFT_ESHAPE (count < 0, numel outside
+ * finite or negative, a beta outside [0, 1), eps not a normal positive
+ * float32, step < 1 without step_dev), GIFT_ESHAPE (count < 0, numel outside
  * [0, 2^34]). */
 gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *tensors,
                             const gift_adamw_options *options);

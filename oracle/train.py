@@ -1,9 +1,9 @@
 """The training step around the codec: embedding lookup and gradient, gradient
 norm, AdamW with float32 and 8-bit moments.
 
-Sums are float64.  AdamW keeps float32 values and rounds once per operation, as
-the step's contract has it, so the moments and their codes are comparable bit
-for bit; :func:`adamw_formula` is the same step in float64 throughout.
+Sums are float64.  AdamW's moments and codes round once per float32 operation,
+as the step's contract has it, so they are comparable bit for bit;
+:func:`adamw_formula` is the step in float64 throughout.
 
 Pins (``tests/test_oracle_train.py``): the lookup's gradient against one-hot
 products and finite differences, one AdamW step against the closed form of the
@@ -76,22 +76,20 @@ def stochastic_codes(x: np.ndarray, r: np.ndarray, keep: bool):
     """E4M3 codes and block scales of float32 values x, rounded by the numbers r."""
     with np.errstate(all="ignore"):
         amax = block_maxima(x)
-        scales = amax / F(448)
-        mult = np.where(amax == 0, F(0), np.minimum(F(448) / amax, np.finfo(F).max)).astype(F)
+        mult = np.where(amax == 0, F(0), np.minimum(F(448) * (F(1) / amax), np.finfo(F).max)).astype(F)
         y = (x * np.repeat(mult, BLOCK)[:x.size]).astype(F)
         a = np.abs(y)
-        # distance to the lower grid point, in 2^-20 of a grid step; below 2^-6 (step 2^-9) y + 2^-6 rounds to
-        # the units of [2^-6, 2^-5)
+        # below 2^-6 (grid step 2^-9) y + 2^-6, rounded to float32, stands for y
         low = a < F(2.0 ** -6)
         t = np.where(low, a + F(2.0 ** -6), a).astype(np.float64)
         step = 2.0 ** (np.floor(np.log2(np.where(np.isfinite(t) & (t > 0), t, 1.0))) - 3)
-        units = np.floor(t / step * 2.0 ** 20) + 16 * r + 8
-        q = np.floor(units / 2.0 ** 20) * step - np.where(low, 2.0 ** -6, 0.0)
+        below = np.floor(t / step)
+        q = (below + (t / step - below + (r + 0.5) / 65536 >= 1)) * step - np.where(low, 2.0 ** -6, 0.0)
         q = np.minimum(q, 448.0)
         if keep:
             q = np.where((q == 0) & (a > 0), 2.0 ** -9, q)
         q = np.where(np.isnan(y), np.nan, np.copysign(q, y))
-    return e4m3.quantize(q.astype(F)), scales.astype(F)
+    return e4m3.quantize(q.astype(F)), (amax * (F(1) / F(448))).astype(F)
 
 
 def decode_moment(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:

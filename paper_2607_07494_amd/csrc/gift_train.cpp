@@ -174,8 +174,8 @@ gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tenso
   if (!o.lr_dev && !(o.lr >= 0.0 && isfinite(o.lr))) return fail(GIFT_EINVAL, call, "lr must be finite and >= 0");
   if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0))
     return fail(GIFT_EINVAL, call, "betas must be in [0, 1)");
-  if (!((float)o.eps > 0.f) || !isfinite((float)o.eps))
-    return fail(GIFT_EINVAL, call, "eps must be a positive float32");
+  if (!((float)o.eps >= 1.17549435e-38f) || !isfinite((float)o.eps))
+    return fail(GIFT_EINVAL, call, "eps must be a normal positive float32");
   if (!o.step_dev && o.step < 1) return fail(GIFT_EINVAL, call, "step must be >= 1");
   if (!aligned(o.lr_dev, 4) || !aligned(o.step_dev, 8) || !aligned(o.grad_scale, 4))
     return fail(GIFT_EINVAL, call, "a device scalar is misaligned");
