@@ -13,7 +13,9 @@ fallback: if ``libgift.so`` is missing, importing this module raises.
 
 from __future__ import annotations
 
+import array
 import ctypes
+import operator
 import os
 import weakref
 
@@ -31,6 +33,7 @@ KERNELS = {
     "embed": 15, "embed_grad": 16, "norm": 17, "optimizer": 18,
 }
 I32, I64 = 0, 1
+_DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
 MOMENTS = {"f32": 0, "e4m3": 1}
 
 _STATUS = {OK: "GIFT_OK", EINVAL: "GIFT_EINVAL", ESHAPE: "GIFT_ESHAPE", ENOMEM: "GIFT_ENOMEM",
@@ -562,10 +565,14 @@ def _index_type(t, name):
 def _on_current_device(**tensors):
     """Raise ValueError unless every tensor is contiguous and on the current device."""
     import torch
+    dev = None
     for name, t in tensors.items():
-        if not t.is_cuda:
+        at = t.get_device()
+        if at < 0:
             raise ValueError(f"{name} must be a GPU tensor")
-        if t.device.index != torch.cuda.current_device():
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if at != dev:
             raise ValueError(f"{name} is on {t.device}, not on the current device")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
@@ -619,20 +626,23 @@ GRAD_NORM_SCRATCH_BYTES = 16384
 
 
 def _gradient_list(grads):
-    """``(dtype, data pointers)`` of a list of gradients on the current device, of one dtype."""
+    """``(dtype, data pointers)`` of a list of gradients on the current device, of one dtype.
+
+    Loops of C functions: a model has hundreds of tensors, and a step's kernels
+    take less time than hundreds of passes through Python."""
     import torch
-    dev, dtype = torch.cuda.current_device(), grads[0].dtype
+    T = torch.Tensor
     dt = _value_dtype(grads[0], "gradients")
-    ptrs = []
-    for g in grads:
-        if g.dtype != dtype:
-            raise TypeError(f"gradients must have one dtype: {g.dtype} and {dtype}")
-        if not g.is_cuda or g.device.index != dev:
-            raise ValueError(f"gradients must be on the current device, not on {g.device}")
-        if not g.is_contiguous():
-            raise ValueError("gradients must be contiguous")
-        ptrs.append(g.data_ptr())
-    return dt, ptrs
+    if len(set(map(_DTYPE, grads))) > 1:
+        raise TypeError(f"gradients must have one dtype: {set(map(_DTYPE, grads))}")
+    devices = set(map(T.get_device, grads))
+    if min(devices) < 0:
+        raise ValueError("gradients must be GPU tensors")
+    if devices != {torch.cuda.current_device()}:
+        raise ValueError(f"gradients must be on the current device, not on {devices}")
+    if not all(map(T.is_contiguous, grads)):
+        raise ValueError("gradients must be contiguous")
+    return dt, array.array("Q", map(T.data_ptr, grads))
 
 
 def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=None):
@@ -648,11 +658,11 @@ def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=
         raise TypeError(f"out must have dtype torch.float32, not {out.dtype}")
     _on_current_device(out=out)
     count = len(grads)
-    dt, ptrs = _gradient_list(grads) if count else (F32, [])
+    dt, ptrs = _gradient_list(grads) if count else (F32, array.array("Q"))
+    sizes = array.array("q", map(torch.Tensor.numel, grads))
     ws, ws_bytes = _scratch(scratch)
-    _check(LIB.gift_grad_norm(ctx.handle, count, (ctypes.c_void_p * count)(*ptrs),
-                              (ctypes.c_int64 * count)(*[g.numel() for g in grads]), dt, max_norm, out.data_ptr(),
-                              ws, ws_bytes))
+    _check(LIB.gift_grad_norm(ctx.handle, count, ptrs.buffer_info()[0], sizes.buffer_info()[0], dt, max_norm,
+                              out.data_ptr(), ws, ws_bytes))
 
 
 class AdamW:
@@ -724,6 +734,10 @@ class AdamW:
                 setattr(x, name, s.data_ptr() + at * s.element_size())
                 if moments == "e4m3":
                     setattr(x, name + "_scales", self.state[name + "_scales"].data_ptr() + at // self.BLOCK * 4)
+        # the tensors' gradient fields, as 64-bit words
+        words = memoryview(self._tensors).cast("B").cast("Q") if count else memoryview(array.array("Q"))
+        self._grad_words = words[_AdamWTensor.grad.offset // 8::ctypes.sizeof(_AdamWTensor) // 8]
+        self._shapes = list(map(_SHAPE, self.params))
         self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
                                       moments=MOMENTS[moments])
 
@@ -758,16 +772,19 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError("grads must have one entry per parameter")
-        for g, p in zip(grads, self.params):
-            if g.shape != p.shape:
-                raise ValueError(f"a gradient must have shape {tuple(p.shape)}, not {tuple(g.shape)}")
+        shapes = list(map(_SHAPE, grads))
+        if shapes != self._shapes:
+            got, want = next((g, p) for g, p in zip(shapes, self._shapes) if g != p)
+            raise ValueError(f"a gradient must have shape {tuple(want)}, not {tuple(got)}")
         o = self._options
+        scalars = {}
         for name, x, dtype in (("lr", lr, torch.float32), ("step", step, torch.int64),
                                ("grad_scale", grad_scale, torch.float32)):
             if isinstance(x, torch.Tensor):
                 if x.dtype != dtype or x.numel() != 1:
                     raise TypeError(f"{name} must be one {dtype} element")
-                _on_current_device(**{name: x})
+                scalars[name] = x
+        _on_current_device(**scalars)
         if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
             raise TypeError("grad_scale must be a tensor")
         on_device = isinstance(step, torch.Tensor)
@@ -777,8 +794,7 @@ class AdamW:
         o.grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
         if grads:
             o.grad_dtype, ptrs = _gradient_list(grads)
-            for x, ptr in zip(self._tensors, ptrs):
-                x.grad = ptr
+            self._grad_words[:] = memoryview(ptrs)
         _check(LIB.gift_adamw_step(self.ctx.handle, len(grads), self._tensors, ctypes.byref(o)))
         if not on_device:
             self.steps = number

@@ -2,7 +2,6 @@
 pointers are never dereferenced, CPU tensors never passed on."""
 
 import ctypes
-import types
 
 import pytest
 import torch
@@ -194,10 +193,10 @@ def test_binding_adamw_step(ctx):
         opt.step([], lr=z(2))
     with pytest.raises(TypeError, match="step must be one"):
         opt.step([], lr=0.1, step=z(1))
-    opt.params = [types.SimpleNamespace(shape=torch.Size([2, 2]))]
+    opt.params, opt._shapes = [z(2, 2)], [torch.Size([2, 2])]
     with pytest.raises(ValueError, match="a gradient must have shape"):
         opt.step([z(4)], lr=0.1)
     with pytest.raises(gift.GiftError, match="lr must be"):
-        opt.params = []
+        opt.params, opt._shapes = [], []
         opt.step([], lr=-1.0)
     assert opt.steps == 0
