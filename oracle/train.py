@@ -43,9 +43,8 @@ def lookup_grad(tokens: np.ndarray, dout: np.ndarray, V: int, scale: float = 1.0
     N, T, d = dout.shape
     out = np.zeros((N, V, d))
     for j in range(N):
-        for t in range(T):
-            if 0 <= tokens[j, t] < V:
-                out[j, tokens[j, t]] += dout[j, t].astype(np.float64)
+        inside = (tokens[j] >= 0) & (tokens[j] < V)
+        np.add.at(out[j], tokens[j][inside], dout[j][inside].astype(np.float64))
     return out * float(scale)
 
 

@@ -4,14 +4,14 @@
 //
 //   grads[j][v] (+)= scale * sum over t with tokens[j][t] = v of dout[j][t]
 //
-// The gradient first orders each rank's positions by token (a stable radix
-// sort, 8 bits a pass), so that a row's terms are neighbours and stand in
-// position order.  The ordered list is cut into runs of kRun entries, one wave
-// each: the work does not depend on how often a token occurs.  A wave adds its
-// entries' rows in float32 and stores every row that begins and ends in its
-// run; the parts of rows that cross a border go to scratch and a second kernel
-// adds them in order.  No atomics on values: the same inputs give the same
-// bits.  Rows without a token are zeroed by further waves of the same launch.
+// The gradient first orders each rank's positions by token (stable radix sort),
+// so that a row's terms are neighbours and stand in position order.  The
+// ordered list is cut into runs of 8 to 32 entries, one wave each: the work
+// does not depend on how often a token occurs.  A wave adds its entries' rows
+// in float32 and stores every row that begins and ends in its run; the parts of
+// rows that cross a border go to scratch and a second kernel adds them in a
+// fixed order.  No atomics on values: the same inputs give the same bits.  Rows
+// without a token are zeroed by further waves of the same launch.
 //
 // Ids outside [0, V) (padding) get the sort key V, the largest: they end up
 // behind all others and nothing reads them.
@@ -191,18 +191,167 @@ __global__ __launch_bounds__(256) void lookup_kernel(const TIn *table, const voi
 // ---------------------------------------------------------------------------
 // Sort of each rank's positions by token
 // ---------------------------------------------------------------------------
+// Ranks of up to kLdsKeys positions are sorted by one workgroup each in LDS, all
+// radix passes in one launch; longer ones through memory, a counting and a
+// scattering launch a pass.
+constexpr int kDigits = 256;
+constexpr int kSmallKeys = 2048, kLdsKeys = 8192;
+
+// lanes of the wave that are `in` and hold the same digit (8 bits) as this one
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool in) {
+  const uint64_t all = __ballot(in);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const uint64_t ones = __ballot((digit >> b) & 1u);
+    const uint32_t own = (uint32_t)__builtin_amdgcn_sbfe((int)digit, b, 1);   // all ones where the bit is set
+    lo &= ~((uint32_t)ones ^ own);
+    hi &= ~((uint32_t)(ones >> 32) ^ own);
+  }
+  return (uint64_t)hi << 32 | lo;
+}
+
+struct LdsSortArgs {
+  const void *tokens;      // [N, T]
+  bool wide;
+  uint32_t *key, *pos;     // [N, T], ordered
+  uint32_t *present;       // null, or [N][words]: bit v % 32 of word v / 32 set where token v occurs
+  int64_t T, V, words;
+  int bits;                // of a key
+};
+
+// One workgroup of WAVES waves sorts one rank; a wave holds up to ITEMS x 64
+// neighbouring keys.  Per pass a wave walks its keys in order: a key's place is
+// the keys before it (in lower digits, earlier waves, earlier steps and lower
+// lanes).  Bound by the chain of counter updates and the vector instructions of
+// one CU; 8 x 2048 keys of 15 bits: 4 waves 14 us, 8 waves 10, 16 waves 9.
+template <int WAVES, int ITEMS>
+__global__ __launch_bounds__(WAVES * 64) void sort_lds_kernel(LdsSortArgs a) {
+  constexpr int kThreads = WAVES * 64, kKeys = kThreads * ITEMS;
+  __shared__ uint32_t keys[kKeys];
+  __shared__ uint16_t places[kKeys];
+  __shared__ uint32_t next[WAVES][kDigits];
+  __shared__ uint32_t digit_sum[4];
+  const int64_t rank = blockIdx.x;
+  const int n = (int)a.T;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const int steps = (n + kThreads - 1) / kThreads, lo = wave * steps * 64;
+  for (int shift = 0; shift < a.bits; shift += 8) {
+    for (int i = threadIdx.x; i < WAVES * kDigits; i += kThreads) next[0][i] = 0;
+    __syncthreads();
+    uint32_t key[ITEMS], where[ITEMS], order[ITEMS];
+    constexpr uint32_t mask = kDigits - 1;
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      if (it >= steps) break;
+      const int i = lo + it * 64 + lane;
+      const bool in = i < n;
+      key[it] = 0;
+      where[it] = 0;
+      if (in) {
+        if (shift == 0) {
+          const int64_t id = read_token(a.tokens, a.wide, rank * a.T + i);
+          key[it] = (uint32_t)(id >= 0 && id < a.V ? id : a.V);
+          where[it] = i;
+        } else {
+          key[it] = keys[i];
+          where[it] = places[i];
+        }
+      }
+    }
+    // the digits' groups first (independent of each other), then the counters' chain
+    uint64_t same[ITEMS];
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it)
+      if (it < steps) same[it] = same_digit((key[it] >> shift) & mask, lo + it * 64 + lane < n);
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      if (it >= steps) break;
+      const bool in = lo + it * 64 + lane < n;
+      const uint32_t digit = (key[it] >> shift) & mask;
+      const int before = __popcll(same[it] & ((1ull << lane) - 1ull));
+      uint32_t seen = 0;
+      if (in) seen = next[wave][digit];
+      __builtin_amdgcn_wave_barrier();
+      if (in && before == 0) next[wave][digit] = seen + (uint32_t)__popcll(same[it]);
+      __builtin_amdgcn_wave_barrier();
+      order[it] = seen + before;
+    }
+    __syncthreads();
+    uint32_t sum = 0, upto = 0;
+    if (threadIdx.x < kDigits) {
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const uint32_t c = next[w][threadIdx.x];
+        next[w][threadIdx.x] = sum;
+        sum += c;
+      }
+      upto = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t t = (uint32_t)__shfl_up((int)upto, o);
+        if (lane >= o) upto += t;
+      }
+      if (lane == 63) digit_sum[wave] = upto;
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) {
+      uint32_t base = upto - sum;
+      for (int w = 0; w < wave; ++w) base += digit_sum[w];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) next[w][threadIdx.x] += base;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      if (it >= steps) break;
+      if (lo + it * 64 + lane >= n) continue;
+      const uint32_t at = next[wave][(key[it] >> shift) & mask] + order[it];
+      keys[at] = key[it];
+      places[at] = (uint16_t)where[it];
+    }
+    __syncthreads();
+  }
+  uint32_t *key_out = a.key + rank * a.T, *pos_out = a.pos + rank * a.T;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    key_out[i] = keys[i];
+    pos_out[i] = places[i];
+  }
+  if (!a.present) return;
+  // the rows that occur, a window of table rows at a time
+  uint32_t *bits = &next[0][0];
+  uint32_t *out = a.present + rank * a.words;
+  for (int64_t word0 = 0; word0 < a.words; word0 += WAVES * kDigits) {
+    for (int i = threadIdx.x; i < WAVES * kDigits; i += kThreads) bits[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const uint32_t k = keys[i];
+      const int64_t w = (int64_t)(k / 32) - word0;
+      if ((int64_t)k < a.V && w >= 0 && w < WAVES * kDigits && (i == 0 || keys[i - 1] != k)) atomicOr(&bits[w], 1u << (k % 32));
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < WAVES * kDigits && word0 + i < a.words; i += kThreads) out[word0 + i] = bits[i];
+    __syncthreads();
+  }
+}
+
 constexpr int kSortThreads = 256;
 constexpr int kSortPerWave = 512;                      // keys of a wave, in order
 constexpr int kSortTile = 4 * kSortPerWave;            // keys of a workgroup
-constexpr int kDigits = 256;
+
+constexpr int kSortItems = kSortTile / kSortThreads;
+// Up to this many tiles a scattering workgroup sums their counts itself (65536
+// positions: a launch between the two took 8.6 us a pass, this adds 1).
+constexpr int kScanTiles = 64;
 
 struct SortArgs {
   const void *tokens;      // first pass: [N, T] ids; else null
-  bool wide;
+  bool wide, scanned;      // scanned: hist holds first places
   const uint32_t *key_in, *pos_in;
   uint32_t *key_out, *pos_out;
-  uint32_t *hist;          // [N][256][tiles]
-  int64_t T, V;
+  uint32_t *hist;          // [N][tiles][256] counts, then first places
+  uint32_t *present;       // null, or [N][words] (LdsSortArgs): cleared by the first pass, set by the second
+  int64_t T, V, words;
   int tiles, shift;
 };
 
@@ -215,119 +364,176 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t rank, in
 __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(SortArgs a) {
   __shared__ uint32_t count[kDigits];
   const int64_t rank = blockIdx.y;
+  uint32_t *present = a.present ? a.present + rank * a.words : nullptr;
+  if (present && a.shift == 0)
+    for (int64_t w = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; w < a.words; w += (int64_t)gridDim.x * kSortThreads)
+      present[w] = 0;
   count[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t lo = (int64_t)blockIdx.x * kSortTile, hi = lo + kSortTile < a.T ? lo + kSortTile : a.T;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads)
-    atomicAdd(&count[(sort_key(a, rank, i) >> a.shift) & 255u], 1u);
+  const int64_t lo = (int64_t)blockIdx.x * kSortTile + threadIdx.x;
+  uint32_t key[kSortItems];
+#pragma unroll
+  for (int it = 0; it < kSortItems; ++it)
+    key[it] = lo + it * kSortThreads < a.T ? sort_key(a, rank, lo + it * kSortThreads) : 0xffffffffu;
+#pragma unroll
+  for (int it = 0; it < kSortItems; ++it) {
+    const uint32_t k = key[it];
+    if (lo + it * kSortThreads >= a.T) continue;
+    atomicAdd(&count[(k >> a.shift) & 255u], 1u);
+    // (a bit already seen as set need not be set again: frequent tokens)
+    if (present && a.shift == 8 && (int64_t)k < a.V && !(present[k / 32] >> (k % 32) & 1u))
+      atomicOr(&present[k / 32], 1u << (k % 32));
+  }
   __syncthreads();
-  a.hist[(rank * kDigits + threadIdx.x) * a.tiles + blockIdx.x] = count[threadIdx.x];
+  a.hist[(rank * a.tiles + blockIdx.x) * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
-// exclusive prefix sums of one rank's [256][tiles] counts, in place
-__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *hist, int tiles) {
-  __shared__ uint32_t wave_sum[16];
-  uint32_t *h = hist + (int64_t)blockIdx.x * kDigits * tiles;
-  const int64_t n = (int64_t)kDigits * tiles;
+// exclusive prefix sums over 256 digits, one a thread
+__device__ __forceinline__ uint32_t digits_before(uint32_t count, uint32_t wave_sum[4]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  uint32_t carry = 0;
-  for (int64_t at = 0; at < n; at += 1024) {
-    const int64_t i = at + threadIdx.x;
-    const uint32_t own = i < n ? h[i] : 0u;
-    uint32_t s = own;
+  uint32_t s = count;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t t = (uint32_t)__shfl_up((int)s, o);
+    if (lane >= o) s += t;
+  }
+  if (lane == 63) wave_sum[wave] = s;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) s += wave_sum[w];
+  return s - count;
+}
+
+// one rank's [tiles][256] counts become first places, in place (many tiles): a
+// digit's tiles in four quarters, eight loads in flight
+__global__ __launch_bounds__(4 * kDigits) void sort_scan_kernel(uint32_t *hist, int tiles) {
+  __shared__ uint32_t quarter_sum[4][kDigits];
+  __shared__ uint32_t wave_sum[4];
+  const int digit = threadIdx.x % kDigits, quarter = threadIdx.x / kDigits, share = (tiles + 3) / 4;
+  const int from = quarter * share, to = from + share < tiles ? from + share : tiles;
+  uint32_t *h = hist + (int64_t)blockIdx.x * tiles * kDigits + digit;
+  uint32_t sum = 0;
+#pragma unroll 8
+  for (int t = from; t < to; ++t) sum += h[(int64_t)t * kDigits];
+  quarter_sum[quarter][digit] = sum;
+  __syncthreads();
+  uint32_t before = 0, total = 0;
+  for (int q = 0; q < 4; ++q) {
+    if (q < quarter) before += quarter_sum[q][digit];
+    total += quarter_sum[q][digit];
+  }
+  __syncthreads();
+  if (quarter == 0) quarter_sum[0][digit] = total;
+  __syncthreads();
+  // every digit's first place, by the first four waves
+  uint32_t at = 0;
+  {
+    const int lane = threadIdx.x & 63, wave = digit / 64;
+    uint32_t s = quarter_sum[0][digit];
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const uint32_t t = (uint32_t)__shfl_up((int)s, o);
       if (lane >= o) s += t;
     }
-    if (lane == 63) wave_sum[wave] = s;
+    if (lane == 63 && quarter == 0) wave_sum[wave] = s;
     __syncthreads();
-    uint32_t before = carry, total = 0;
+    for (int w = 0; w < wave; ++w) s += wave_sum[w];
+    at = s - quarter_sum[0][digit] + before;
+  }
+  for (int t0 = from; t0 < to; t0 += 8) {
+    uint32_t c[8];
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) before += wave_sum[w];
-      total += wave_sum[w];
+    for (int u = 0; u < 8; ++u) c[u] = t0 + u < to ? h[(int64_t)(t0 + u) * kDigits] : 0u;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (t0 + u < to) h[(int64_t)(t0 + u) * kDigits] = at;
+      at += c[u];
     }
-    if (i < n) h[i] = before + s - own;
-    carry += total;
-    __syncthreads();
   }
-}
-
-// lanes of the wave that are `in` and hold the same digit as this one
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool in) {
-  uint64_t m = __ballot(in);
-#pragma unroll
-  for (int b = 0; b < 8; ++b) {
-    const uint64_t ones = __ballot((digit >> b) & 1u);
-    m &= (digit >> b) & 1u ? ones : ~ones;
-  }
-  return m;
 }
 
 // Stable scatter: a wave walks its 512 keys in order, 64 at a time; a key's
 // place is its digit's next free place plus the equal digits in lower lanes.
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) {
   __shared__ uint32_t next[4][kDigits];
+  __shared__ uint32_t wave_sum[4];
   const int64_t rank = blockIdx.y;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
 #pragma unroll
   for (int w = 0; w < 4; ++w) next[w][threadIdx.x] = 0;
-  __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * kSortTile + wave * kSortPerWave;
-  uint32_t key[kSortPerWave / 64];
+  uint32_t key[kSortItems], pos[kSortItems];
 #pragma unroll
-  for (int it = 0; it < kSortPerWave / 64; ++it) {
+  for (int it = 0; it < kSortItems; ++it) {
     const int64_t i = lo + it * 64 + lane;
     key[it] = i < a.T ? sort_key(a, rank, i) : 0u;
-    if (i < a.T) atomicAdd(&next[wave][(key[it] >> a.shift) & 255u], 1u);
+    pos[it] = a.tokens || i >= a.T ? (uint32_t)i : a.pos_in[rank * a.T + i];
+  }
+  // the tile's first place of digit threadIdx.x
+  const uint32_t *h = a.hist + rank * a.tiles * kDigits + threadIdx.x;
+  uint32_t first;
+  if (a.scanned) {
+    first = h[(int64_t)blockIdx.x * kDigits];
+  } else {
+    uint32_t total = 0;
+    first = 0;
+    for (int t = 0; t < a.tiles; ++t) {
+      const uint32_t c = h[(int64_t)t * kDigits];
+      if (t < (int)blockIdx.x) first += c;
+      total += c;
+    }
+    first += digits_before(total, wave_sum);
   }
   __syncthreads();
-  uint32_t at = a.hist[(rank * kDigits + threadIdx.x) * a.tiles + blockIdx.x];
+  uint64_t same[kSortItems];
+  uint32_t order[kSortItems];
+#pragma unroll
+  for (int it = 0; it < kSortItems; ++it) same[it] = same_digit((key[it] >> a.shift) & 255u, lo + it * 64 + lane < a.T);
+#pragma unroll
+  for (int it = 0; it < kSortItems; ++it) {
+    const bool in = lo + it * 64 + lane < a.T;
+    const uint32_t digit = (key[it] >> a.shift) & 255u;
+    const int before = __popcll(same[it] & ((1ull << lane) - 1ull));
+    uint32_t seen = 0;
+    if (in) seen = next[wave][digit];
+    __builtin_amdgcn_wave_barrier();
+    if (in && before == 0) next[wave][digit] = seen + (uint32_t)__popcll(same[it]);
+    __builtin_amdgcn_wave_barrier();
+    order[it] = seen + before;
+  }
+  __syncthreads();
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const uint32_t c = next[w][threadIdx.x];
-    next[w][threadIdx.x] = at;
-    at += c;
+    next[w][threadIdx.x] = first;
+    first += c;
   }
   __syncthreads();
   uint32_t *key_out = a.key_out + rank * a.T, *pos_out = a.pos_out + rank * a.T;
 #pragma unroll
-  for (int it = 0; it < kSortPerWave / 64; ++it) {
-    const int64_t i = lo + it * 64 + lane;
-    const bool in = i < a.T;
-    const uint32_t digit = (key[it] >> a.shift) & 255u;
-    const uint64_t same = same_digit(digit, in);
-    const int before = __popcll(same & ((1ull << lane) - 1ull));
-    uint32_t place = 0;
-    if (in) place = next[wave][digit] + before;
-    __builtin_amdgcn_wave_barrier();
-    if (in && before == 0) next[wave][digit] += (uint32_t)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
-    if (in) {
-      key_out[place] = key[it];
-      pos_out[place] = a.tokens ? (uint32_t)i : a.pos_in[rank * a.T + i];
-    }
+  for (int it = 0; it < kSortItems; ++it) {
+    if (lo + it * 64 + lane >= a.T) continue;
+    const uint32_t place = next[wave][(key[it] >> a.shift) & 255u] + order[it];
+    key_out[place] = key[it];
+    pos_out[place] = pos[it];
   }
 }
 
 // ---------------------------------------------------------------------------
 // Sums over the ordered positions
 // ---------------------------------------------------------------------------
-constexpr int kRun = 32;          // ordered entries of one wave
 constexpr int kZeroRows = 64;     // table rows looked over by one wave
-constexpr int kInFlight = 8;      // rows loaded ahead
 
 struct SumArgs {
   const uint32_t *key, *pos;   // [N][T], ordered by (key, pos)
   const void *dout;            // [N][T][d]
   float *grads;                // [N][V][d]
   float *part;                 // [N][runs][2][d4]: a run's first row, where it began before; its last, where it goes on
-  int64_t T, V, d, d4;
+  const uint32_t *present;     // null, or [N][words] (LdsSortArgs)
+  int64_t T, V, d, d4, words;
   int64_t runs, chunks, run_waves;
   int64_t zero_groups, zero_ranks;   // waves behind run_waves: zero_ranks x zero_groups
+  int run;                           // ordered entries of one wave, at most 64
   float scale;
-  bool accumulate;
 };
 
 // the lane's own columns to p
@@ -342,45 +548,35 @@ __device__ __forceinline__ void keep_row(float *p, const Columns<VEC> &c, const 
   }
 }
 
-template <int VEC>
-__device__ __forceinline__ void write_grad(const SumArgs &a, int64_t rank, uint32_t row, const Columns<VEC> &c,
-                                           const float sum[VEC]) {
-  if (!c.any) return;
-  float *p = a.grads + ((int64_t)rank * a.V + row) * a.d + c.first;
-  float v[VEC];
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) v[k] = sum[k] * a.scale;
-  if (a.accumulate) {
-    float old[VEC];
-    load_row<VEC>(p, old);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) v[k] = old[k] + v[k];
-  }
-  keep_row<VEC>(p, c, v);
-}
-
 // n consecutive floats set to zero by one wave
 __device__ __forceinline__ void zero_span(float *p, int64_t n) {
   const int lane = threadIdx.x & 63;
   const int64_t n4 = n / 4;
-  for (int64_t i = lane; i < n4; i += 64) *reinterpret_cast<floatx4_u *>(p + 4 * i) = floatx4_u{0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = lane; i < n4; i += 64)
+    __builtin_nontemporal_store(floatx4_u{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<floatx4_u *>(p + 4 * i));
   if (lane < n - 4 * n4) p[4 * n4 + lane] = 0.f;
 }
 
-// rows without a token among kZeroRows neighbours: each lane looks one up by
-// bisection, neighbouring empty rows are cleared as one span
+// rows without a token among kZeroRows neighbours, from the sort's bits or
+// else by a bisection a lane; neighbouring empty rows are cleared as one span
 __device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_t group) {
   const int lane = threadIdx.x & 63;
   const int64_t row0 = group * kZeroRows, row = row0 + lane;
-  const uint32_t *key = a.key + rank * a.T;
-  int64_t lo = 0, hi = a.T;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if ((int64_t)key[mid] < row) lo = mid + 1;
-    else hi = mid;
+  uint64_t left;
+  if (a.present) {
+    const uint32_t *words = a.present + rank * a.words + 2 * group;
+    const uint64_t there = (uint64_t)words[0] | (2 * group + 1 < a.words ? (uint64_t)words[1] << 32 : 0ull);
+    left = ~there & (a.V - row0 < 64 ? (1ull << (a.V - row0)) - 1ull : ~0ull);
+  } else {
+    const uint32_t *key = a.key + rank * a.T;
+    int64_t lo = 0, hi = a.T;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if ((int64_t)key[mid] < row) lo = mid + 1;
+      else hi = mid;
+    }
+    left = __ballot(row < a.V && !(lo < a.T && (int64_t)key[lo] == row));
   }
-  const bool empty = row < a.V && !(lo < a.T && (int64_t)key[lo] == row);
-  uint64_t left = __ballot(empty);
   float *base = a.grads + (rank * a.V + row0) * a.d;
   while (left) {
     const int s = __ffsll((unsigned long long)left) - 1;
@@ -391,10 +587,12 @@ __device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_
   }
 }
 
-template <typename TIn, int VEC>
+// ACC: what grads holds of a row is loaded with the row's first entry.
+template <typename TIn, int VEC, bool ACC>
 __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
+  constexpr int kInFlight = ACC ? 4 : 8;      // rows loaded ahead
   const int lane = threadIdx.x & 63;
-  int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (w >= a.run_waves) {
     w -= a.run_waves;
     const int64_t rank = w / a.zero_groups;
@@ -403,95 +601,140 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
   }
   const int64_t chunk = w % a.chunks, r = w / a.chunks, rank = r / a.runs, run = r - rank * a.runs;
   const uint32_t *key = a.key + rank * a.T, *pos = a.pos + rank * a.T;
-  const int64_t lo = run * kRun, hi = lo + kRun < a.T ? lo + kRun : a.T;
+  const int64_t lo = run * a.run, hi = lo + a.run < a.T ? lo + a.run : a.T;
   const int64_t mine = lo + lane < hi ? lo + lane : hi - 1;
   const uint32_t my_key = key[mine], my_pos = pos[mine];
+  const uint32_t key_before = lo > 0 ? key[lo - 1] : 0xffffffffu, key_behind = hi < a.T ? key[hi] : 0xffffffffu;
   // entries of ids inside the table come first
   const int count = __popcll(__ballot(lo + lane < hi && (int64_t)my_key < a.V));
   if (count == 0) return;
   const Columns<VEC> c(chunk, a.d);
   const TIn *dout = static_cast<const TIn *>(a.dout) + rank * a.T * a.d + c.first;
-  const uint32_t first_key = __builtin_amdgcn_readlane(my_key, 0);
-  const bool begun = lo > 0 && key[lo - 1] == first_key;
-  const bool goes_on = count == hi - lo && hi < a.T && key[hi] == (uint32_t)__builtin_amdgcn_readlane(my_key, count - 1);
-  float *part = a.part + ((rank * a.runs + run) * 2) * a.d4;
-  auto flush = [&](uint32_t row, bool head, bool tail, const float sum[VEC]) {
+  float *grads = a.grads + rank * a.V * a.d + c.first;
+  float *part = a.part + ((rank * a.runs + run) * 2) * a.d4 + c.first;
+  uint32_t row = __builtin_amdgcn_readlane(my_key, 0);
+  bool head = key_before == row;
+  // the run's last row goes on behind it (key V never does: an id outside the table is not counted)
+  const bool goes_on = count == hi - lo && key_behind == (uint32_t)__builtin_amdgcn_readlane(my_key, count - 1);
+  float sum[VEC], old[VEC];
+  auto flush = [&](bool tail) {
+    if (!c.any) return;
     if (head || tail) {
-      if (!c.any) return;
-      keep_row<VEC>(part + (head ? 0 : a.d4) + c.first, c, sum);
-    } else {
-      write_grad<VEC>(a, rank, row, c, sum);
+      keep_row<VEC>(part + (head ? 0 : a.d4), c, sum);
+      return;
     }
-  };
-  float sum[VEC];
+    float v[VEC];
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
-  uint32_t row = first_key;
-  bool head = begun;
+    for (int e = 0; e < VEC; ++e) v[e] = ACC ? old[e] + sum[e] * a.scale : sum[e] * a.scale;
+    keep_row<VEC>(grads + (int64_t)row * a.d, c, v);
+  };
   for (int i0 = 0; i0 < count; i0 += kInFlight) {
-    float x[kInFlight][VEC];
+    float x[kInFlight][VEC], was[ACC ? kInFlight : 1][VEC];
+    uint32_t k[kInFlight];
+    bool starts[kInFlight];
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       const int i = i0 + u < count ? i0 + u : count - 1;
+      k[u] = (uint32_t)__builtin_amdgcn_readlane(my_key, i);
+      starts[u] = i0 + u < count && (i == 0 || k[u] != (uint32_t)__builtin_amdgcn_readlane(my_key, i > 0 ? i - 1 : 0));
       const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(my_pos, i);
       if (c.any) load_row<VEC>(dout + (int64_t)p * a.d, x[u]);
+      if constexpr (ACC)
+        if (starts[u] && c.any) load_row<VEC>(grads + (int64_t)k[u] * a.d, was[u]);
     }
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (i0 + u >= count) break;
-      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(my_key, i0 + u);
-      if (k != row) {
-        flush(row, head, false, sum);
-        head = false;
-        row = k;
+      if (starts[u]) {
+        if (i0 + u > 0) {
+          flush(false);
+          head = false;
+        }
+        row = k[u];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+        for (int e = 0; e < VEC; ++e) {
+          sum[e] = 0.f;
+          if constexpr (ACC) old[e] = was[u][e];
+        }
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) sum[e] += x[u][e];
     }
   }
-  flush(row, head, goes_on, sum);
+  flush(goes_on);
 }
 
 // Rows that cross a run's border: the run where such a row begins adds the
-// parts of the following runs, in order.
-template <int VEC>
+// parts of the following runs, in order; of more than kJoinAlone parts the
+// workgroup's four waves add a quarter each, then the quarters' sums.
+constexpr int kJoinAlone = 8;
+
+template <int VEC, bool ACC>
 __global__ __launch_bounds__(256) void embgrad_join_kernel(SumArgs a) {
-  const int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (w >= a.run_waves) return;
+  __shared__ float quarter[4][64][VEC];
+  constexpr int kInFlight = 8;
+  const int64_t w = blockIdx.x;
   const int64_t chunk = w % a.chunks, r = w / a.chunks, rank = r / a.runs, run = r - rank * a.runs;
   const uint32_t *key = a.key + rank * a.T;
-  const int64_t lo = run * kRun, hi = lo + kRun;
+  const int64_t lo = run * a.run, hi = lo + a.run;
   if (hi >= a.T) return;
   const uint32_t row = key[hi - 1];
   if ((int64_t)row >= a.V || key[hi] != row) return;                     // nothing goes on
   if (key[lo] == row && lo > 0 && key[lo - 1] == row) return;            // begun in an earlier run
-  // the last entry of this row
-  int64_t b = hi, e = a.T;
+  // the runs behind this one that the row reaches: the end of its entries, by steps of a growing length, then bisection
+  int64_t b = hi, e = hi + a.run;
+  while (e < a.T && key[e] == row) {
+    b = e;
+    e += 2 * (e - hi);
+  }
+  e = e < a.T ? e : a.T;
   while (b < e) {
     const int64_t mid = (b + e) / 2;
     if (key[mid] <= row) b = mid + 1;
     else e = mid;
   }
-  const int64_t last = (b - 1) / kRun;
+  const int64_t last = (b - 1) / a.run, n = last - run;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const bool alone = n <= kJoinAlone;
+  if (alone && wave > 0) return;
   const Columns<VEC> c(chunk, a.d);
-  if (!c.any) return;
-  const float *part = a.part + rank * a.runs * 2 * a.d4 + c.first;
+  const float *part = a.part + (rank * a.runs + run) * 2 * a.d4 + c.first;
+  const int64_t share = alone ? n : (n + 3) / 4;
+  const int64_t from = 1 + wave * share, to = from + share < n + 1 ? from + share : n + 1;
   float sum[VEC];
-  load_row<VEC>(part + (run * 2 + 1) * a.d4, sum);
-  for (int64_t u0 = run + 1; u0 <= last; u0 += kInFlight) {
-    float x[kInFlight][VEC];
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) load_row<VEC>(part + (u0 + u <= last ? u0 + u : last) * 2 * a.d4, x[u]);
+  for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
+  if (c.any) {
+    if (wave == 0) load_row<VEC>(part + a.d4, sum);
+    for (int64_t u0 = from; u0 < to; u0 += kInFlight) {
+      float x[kInFlight][VEC];
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      if (u0 + u > last) break;
+      for (int u = 0; u < kInFlight; ++u) load_row<VEC>(part + (u0 + u < to ? u0 + u : to - 1) * 2 * a.d4, x[u]);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) sum[k] += x[u][k];
+      for (int u = 0; u < kInFlight; ++u) {
+        if (u0 + u >= to) break;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) sum[k] += x[u][k];
+      }
     }
   }
-  write_grad<VEC>(a, rank, row, c, sum);
+  if (!alone) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) quarter[wave][lane][k] = sum[k];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int q = 1; q < 4; ++q)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) sum[k] += quarter[q][lane][k];
+  }
+  if (!c.any) return;
+  float *p = a.grads + (rank * a.V + row) * a.d + c.first;
+  float v[VEC], old[VEC];
+  if constexpr (ACC) load_row<VEC>(p, old);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) v[k] = ACC ? old[k] + sum[k] * a.scale : sum[k] * a.scale;
+  keep_row<VEC>(p, c, v);
 }
 
 unsigned blocks_for(int64_t waves) { return (unsigned)((waves + 3) / 4); }
@@ -507,28 +750,41 @@ int64_t column_chunks(int64_t d) {
 
 size_t a256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+// Ordered entries of a wave: 32 where that still makes two waves a SIMD, down
+// to 8 for short ranks, whose time is the longest chain of additions.
+int run_length(int64_t N, int64_t T, int64_t d) {
+  int run = 32;
+  while (run > 8 && N * ((T + run - 1) / run) * column_chunks(d) < 2048) run /= 2;
+  return run;
+}
+
 struct GradPlan {
-  size_t key[2], pos[2], hist, part, bytes;
-  int64_t runs, d4;
-  int tiles;
+  size_t key[2], pos[2], hist, part, present, bytes;
+  int64_t runs, d4, words;      // words: of a rank's row bits, 0 without
+  int run, tiles;               // tiles: 0 for the sort in LDS
 };
 
 GradPlan grad_plan(int64_t N, int64_t T, int64_t V, int64_t d) {
   GradPlan p{};
-  p.tiles = (int)((T + kSortTile - 1) / kSortTile);
-  p.runs = (T + kRun - 1) / kRun;
+  p.run = run_length(N, T, d);
+  p.runs = (T + p.run - 1) / p.run;
   p.d4 = (d + 3) / 4 * 4;
+  p.tiles = T <= kLdsKeys ? 0 : (int)((T + kSortTile - 1) / kSortTile);
+  // (past 2^20 rows the windows of the sort in LDS would take longer than the
+  // bisections; a sort of one pass has no second one that sets them)
+  p.words = V <= 1 << 20 && (V >= 256 || p.tiles == 0) ? (V + 31) / 32 : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
     at += a256(bytes);
     return o;
   };
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < (p.tiles ? 2 : 1); ++i) {
     p.key[i] = take((size_t)N * T * 4);
     p.pos[i] = take((size_t)N * T * 4);
   }
   p.hist = take((size_t)N * kDigits * p.tiles * 4);
+  p.present = take((size_t)N * p.words * 4);
   p.part = take((size_t)N * p.runs * 2 * p.d4 * 4);
   p.bytes = at;
   return p;
@@ -553,22 +809,78 @@ void lookup_launch(gift_ctx *ctx, const LookupJob &j) {
 #undef GIFT_LOOKUP
 }
 
-template <typename TIn, int VEC>
-gift_status sum_launch(gift_ctx *ctx, const SumArgs &a, int64_t zero_waves) {
-  hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC>), dim3(blocks_for(a.run_waves + zero_waves)), dim3(256), 0,
-                     ctx->stream, a);
+template <typename TIn, int VEC, bool ACC>
+gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
+  const int64_t waves = a.run_waves + a.zero_ranks * a.zero_groups;
+  hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC, ACC>), dim3(blocks_for(waves)), dim3(256), 0, ctx->stream, a);
   gift_status st = check_launch("embgrad_sum_kernel");
   if (st != GIFT_OK || a.runs < 2) return st;
-  hipLaunchKernelGGL((embgrad_join_kernel<VEC>), dim3(blocks_for(a.run_waves)), dim3(256), 0, ctx->stream, a);
+  hipLaunchKernelGGL((embgrad_join_kernel<VEC, ACC>), dim3((unsigned)a.run_waves), dim3(256), 0, ctx->stream, a);
   return check_launch("embgrad_join_kernel");
 }
 
-template <typename TIn>
-gift_status sum_launch(gift_ctx *ctx, const SumArgs &a, int64_t zero_waves, int vec) {
-  if (vec == 8) return sum_launch<TIn, 8>(ctx, a, zero_waves);
-  if (vec == 4) return sum_launch<TIn, 4>(ctx, a, zero_waves);
-  if (vec == 2) return sum_launch<TIn, 2>(ctx, a, zero_waves);
-  return sum_launch<TIn, 1>(ctx, a, zero_waves);
+template <typename TIn, bool ACC>
+gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
+  const int vec = lane_columns(a.d);
+  if (vec == 8) return sum_launch<TIn, 8, ACC>(ctx, a);
+  if (vec == 4) return sum_launch<TIn, 4, ACC>(ctx, a);
+  if (vec == 2) return sum_launch<TIn, 2, ACC>(ctx, a);
+  return sum_launch<TIn, 1, ACC>(ctx, a);
+}
+
+// Orders every rank's positions; `cur` receives the buffers (0 or 1) with the result.
+gift_status sort_launch(gift_ctx *ctx, const EmbGradJob &j, const GradPlan &p, uint32_t *const key[2],
+                        uint32_t *const pos[2], char *ws, int *cur) {
+  int bits = 0;
+  while ((j.V >> bits) != 0) ++bits;   // the keys are 0 .. V
+  gift_status st;
+  uint32_t *present = p.words && !j.accumulate ? reinterpret_cast<uint32_t *>(ws + p.present) : nullptr;
+  *cur = 0;
+  if (p.tiles == 0) {
+    LdsSortArgs a{};
+    a.tokens = j.tokens;
+    a.wide = j.wide;
+    a.key = key[0];
+    a.pos = pos[0];
+    a.present = present;
+    a.T = j.T;
+    a.V = j.V;
+    a.words = p.words;
+    a.bits = bits;
+    if (j.T <= kSmallKeys)
+      hipLaunchKernelGGL((sort_lds_kernel<16, kSmallKeys / 1024>), dim3(j.N), dim3(1024), 0, ctx->stream, a);
+    else
+      hipLaunchKernelGGL((sort_lds_kernel<16, kLdsKeys / 1024>), dim3(j.N), dim3(1024), 0, ctx->stream, a);
+    return check_launch("sort_lds_kernel");
+  }
+  SortArgs s{};
+  s.hist = reinterpret_cast<uint32_t *>(ws + p.hist);
+  s.present = present;
+  s.T = j.T;
+  s.V = j.V;
+  s.words = p.words;
+  s.tiles = p.tiles;
+  s.scanned = p.tiles > kScanTiles;
+  const dim3 grid(p.tiles, j.N);
+  for (int shift = 0; shift < bits; shift += 8) {
+    s.tokens = shift ? nullptr : j.tokens;
+    s.wide = j.wide;
+    s.key_in = key[*cur];
+    s.pos_in = pos[*cur];
+    *cur = shift ? 1 - *cur : 0;
+    s.key_out = key[*cur];
+    s.pos_out = pos[*cur];
+    s.shift = shift;
+    hipLaunchKernelGGL(sort_hist_kernel, grid, dim3(kSortThreads), 0, ctx->stream, s);
+    if ((st = check_launch("sort_hist_kernel")) != GIFT_OK) return st;
+    if (s.scanned) {
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(j.N), dim3(4 * kDigits), 0, ctx->stream, s.hist, p.tiles);
+      if ((st = check_launch("sort_scan_kernel")) != GIFT_OK) return st;
+    }
+    hipLaunchKernelGGL(sort_scatter_kernel, grid, dim3(kSortThreads), 0, ctx->stream, s);
+    if ((st = check_launch("sort_scatter_kernel")) != GIFT_OK) return st;
+  }
+  return GIFT_OK;
 }
 
 }  // namespace
@@ -590,66 +902,45 @@ size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d) {
 }
 
 int64_t embgrad_waves(const EmbGradJob &j) {
-  const int64_t run = (int64_t)j.N * ((j.T + kRun - 1) / kRun) * column_chunks(j.d);
-  return run + (j.accumulate ? 0 : (int64_t)j.N * ((j.V + kZeroRows - 1) / kZeroRows));
+  // a join takes a workgroup where the sum takes a wave
+  const int64_t run = (int64_t)j.N * ((j.T + run_length(j.N, j.T, j.d) - 1) / run_length(j.N, j.T, j.d)) * column_chunks(j.d);
+  return 4 * run + (j.accumulate ? 0 : (int64_t)j.N * ((j.V + kZeroRows - 1) / kZeroRows));
 }
 
 gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &j, char *ws) {
-  const GradPlan p = grad_plan(j.N, j.T, j.V, j.d);
+  const GradPlan p = j.T > 0 ? grad_plan(j.N, j.T, j.V, j.d) : GradPlan{};
   uint32_t *key[2], *pos[2];
   for (int i = 0; i < 2; ++i) {
     key[i] = reinterpret_cast<uint32_t *>(ws + p.key[i]);
     pos[i] = reinterpret_cast<uint32_t *>(ws + p.pos[i]);
   }
   ProfileScope prof(ctx, GIFT_KERNEL_EMBED_GRAD);
-  gift_status st;
   int cur = 0;
   if (j.T > 0) {
-    int bits = 0;
-    while ((j.V >> bits) != 0) ++bits;   // the keys are 0 .. V
-    SortArgs s{};
-    s.hist = reinterpret_cast<uint32_t *>(ws + p.hist);
-    s.T = j.T;
-    s.V = j.V;
-    s.tiles = p.tiles;
-    const dim3 grid(p.tiles, j.N);
-    for (int shift = 0; shift < bits; shift += 8) {
-      s.tokens = shift ? nullptr : j.tokens;
-      s.wide = j.wide;
-      s.key_in = key[cur];
-      s.pos_in = pos[cur];
-      cur = shift ? 1 - cur : 0;
-      s.key_out = key[cur];
-      s.pos_out = pos[cur];
-      s.shift = shift;
-      hipLaunchKernelGGL(sort_hist_kernel, grid, dim3(kSortThreads), 0, ctx->stream, s);
-      if ((st = check_launch("sort_hist_kernel")) != GIFT_OK) return st;
-      hipLaunchKernelGGL(sort_scan_kernel, dim3(j.N), dim3(1024), 0, ctx->stream, s.hist, p.tiles);
-      if ((st = check_launch("sort_scan_kernel")) != GIFT_OK) return st;
-      hipLaunchKernelGGL(sort_scatter_kernel, grid, dim3(kSortThreads), 0, ctx->stream, s);
-      if ((st = check_launch("sort_scatter_kernel")) != GIFT_OK) return st;
-    }
+    gift_status st = sort_launch(ctx, j, p, key, pos, ws, &cur);
+    if (st != GIFT_OK) return st;
   }
-  const int vec = lane_columns(j.d);
   SumArgs a{};
   a.key = key[cur];
   a.pos = pos[cur];
   a.dout = j.dout;
   a.grads = j.grads;
   a.part = reinterpret_cast<float *>(ws + p.part);
+  a.present = p.words ? reinterpret_cast<const uint32_t *>(ws + p.present) : nullptr;
   a.T = j.T;
   a.V = j.V;
   a.d = j.d;
   a.d4 = p.d4;
+  a.words = p.words;
+  a.run = p.run;
   a.runs = p.runs;
   a.chunks = column_chunks(j.d);
   a.run_waves = (int64_t)j.N * p.runs * a.chunks;
   a.zero_groups = (j.V + kZeroRows - 1) / kZeroRows;
-  a.scale = j.scale;
-  a.accumulate = j.accumulate;
   a.zero_ranks = j.accumulate ? 0 : j.N;
-  const int64_t zero_waves = a.zero_ranks * a.zero_groups;
-  return j.bf16 ? sum_launch<uint16_t>(ctx, a, zero_waves, vec) : sum_launch<float>(ctx, a, zero_waves, vec);
+  a.scale = j.scale;
+  if (j.accumulate) return j.bf16 ? sum_launch<uint16_t, true>(ctx, a) : sum_launch<float, true>(ctx, a);
+  return j.bf16 ? sum_launch<uint16_t, false>(ctx, a) : sum_launch<float, false>(ctx, a);
 }
 
 }  // namespace gift

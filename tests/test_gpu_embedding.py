@@ -2,12 +2,13 @@
 
 The lookup multiplies once in float32 and rounds once to its output type: equal
 to the oracle bit for bit.  The gradient of a row with L terms is a sum of
-float32 additions: every term passes through at most RUN additions of its run,
-the additions of ceil(L / RUN) + 1 run sums, one multiplication by the scale
-and, with accumulate, one addition; each rounding is off by at most 2^-24 of a
-partial sum, and no partial sum exceeds the sum S of the terms' magnitudes:
+float32 additions: every term passes through the additions of its run (8 to 32
+entries, at most RUN = 64), those of the row's at most L / 8 + 2 run sums, one
+multiplication by the scale and, with accumulate, one addition; each rounding
+is off by at most 2^-24 of a partial sum, and no partial sum exceeds the sum S
+of the terms' magnitudes:
 
-    |error| <= (RUN + L / RUN + 4) 2^-24 (scale S + |old|),  RUN = 64
+    |error| <= (RUN + L / 8 + 4) 2^-24 (scale S + |old|)
 """
 
 import numpy as np
@@ -145,6 +146,20 @@ CASES = [
     (1, 20000, 32000, 64, "bf16", 64, "zipf"),
     (1, 9000, 11, 33, "f32", 64, "one"),
     (17, 130, 90, 48, "bf16", 32, "outside"),
+    # the borders of the sort's forms: 2048 and 8192 positions in a workgroup, 64 tiles of 2048, more
+    (2, 8192, 300, 20, "f32", 64, "zipf"),
+    (2, 8193, 3000, 24, "bf16", 32, "outside"),
+    (1, 65536, 2000, 16, "bf16", 64, "zipf"),
+    (1, 40000, 9, 12, "f32", 64, "one"),
+    (1, 30000, 255, 12, "f32", 64, "zipf"),
+    (1, 30000, 256, 12, "f32", 32, "few"),
+    (1, 131072, 700, 8, "bf16", 64, "few"),
+    (2, 131073, 65536, 4, "f32", 64, "outside"),
+    (1, 600_000, 70000, 2, "f32", 32, "zipf"),
+    (1, 300, 1_048_577, 3, "f32", 64, "zipf"),
+    (1, 300, 1_048_576, 3, "f32", 64, "outside"),
+    (2, 5000, 140_000, 9, "bf16", 64, "outside"),
+    (1, 9000, 3, 1030, "bf16", 64, "one"),
 ]
 
 
@@ -170,7 +185,7 @@ def check_grad(got, tok, dout, V, scale, old):
         np.add.at(terms[j, :, 0], t, 1)
     before = old.double().numpy() if old is not None else np.zeros_like(want)
     err = np.abs(got.double().numpy() - (want + before))
-    bound = (RUN + terms / RUN + 4) * 2.0 ** -24 * (size + np.abs(before))
+    bound = (RUN + terms / 8 + 4) * 2.0 ** -24 * (size + np.abs(before))
     assert np.all(err <= bound), float((err - bound).max())
     empty = np.broadcast_to(terms == 0, want.shape)
     np.testing.assert_array_equal(got.numpy()[empty], before[empty])     # zeros, or what was there
@@ -242,7 +257,7 @@ def test_gradient_is_the_lookups_difference_quotient(ctx):
         f.append(float((out.double() * dout.double()).sum()))
         size += float((out.double() * dout.double()).abs().sum())
     terms = torch.bincount(tok[0][(tok[0] >= 0) & (tok[0] < V)], minlength=V).max()
-    slack = 2.0 ** -24 * size + (RUN + float(terms) / RUN + 4) * 2.0 ** -24 * s * float(
+    slack = 2.0 ** -24 * size + (RUN + float(terms) / 8 + 4) * 2.0 ** -24 * s * float(
         (dout[0].double().abs()[(tok[0] >= 0) & (tok[0] < V)] * D.double().abs()[tok[0][(tok[0] >= 0) & (tok[0] < V)]]).sum())
     assert abs((f[0] - f[1]) / 2 - float((grads[0].double() * D.double()).sum())) <= slack
 
