@@ -476,10 +476,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
   } else {
     uint32_t total = 0;
     first = 0;
-    for (int t = 0; t < a.tiles; ++t) {
-      const uint32_t c = h[(int64_t)t * kDigits];
-      if (t < (int)blockIdx.x) first += c;
-      total += c;
+    for (int t0 = 0; t0 < a.tiles; t0 += 16) {
+      uint32_t c[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) c[u] = t0 + u < a.tiles ? h[(int64_t)(t0 + u) * kDigits] : 0u;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        if (t0 + u < (int)blockIdx.x) first += c[u];
+        total += c[u];
+      }
     }
     first += digits_before(total, wave_sum);
   }
@@ -521,8 +526,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
 // ---------------------------------------------------------------------------
 // Sums over the ordered positions
 // ---------------------------------------------------------------------------
-constexpr int kZeroRows = 64;     // table rows looked over by one wave
-
 struct SumArgs {
   const uint32_t *key, *pos;   // [N][T], ordered by (key, pos)
   const void *dout;            // [N][T][d]
@@ -533,6 +536,7 @@ struct SumArgs {
   int64_t runs, chunks, run_waves;
   int64_t zero_groups, zero_ranks;   // waves behind run_waves: zero_ranks x zero_groups
   int run;                           // ordered entries of one wave, at most 64
+  int zero_rows;                     // table rows looked over by one wave, a power of two up to 32
   float scale;
 };
 
@@ -548,25 +552,30 @@ __device__ __forceinline__ void keep_row(float *p, const Columns<VEC> &c, const 
   }
 }
 
-// n consecutive floats set to zero by one wave
+// n consecutive floats set to zero by one wave: whole 128-byte lines past the
+// caches, what is left at either end through them (streamed parts of lines
+// cost their whole line: 3 x 50001 rows of 771 109 us, now 95)
 __device__ __forceinline__ void zero_span(float *p, int64_t n) {
   const int lane = threadIdx.x & 63;
-  const int64_t n4 = n / 4;
-  for (int64_t i = lane; i < n4; i += 64)
-    __builtin_nontemporal_store(floatx4_u{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<floatx4_u *>(p + 4 * i));
-  if (lane < n - 4 * n4) p[4 * n4 + lane] = 0.f;
+  const int64_t lead = (-(int64_t)(reinterpret_cast<uintptr_t>(p) / 4)) & 31, skip = lead < n ? lead : n;
+  if (lane < skip) p[lane] = 0.f;
+  p += skip;
+  n -= skip;
+  const int64_t whole = n & ~31ll;
+  for (int64_t i = lane * 4; i < whole; i += 256)
+    __builtin_nontemporal_store(floatx4_u{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<floatx4_u *>(p + i));
+  if (lane < n - whole) p[whole + lane] = 0.f;
 }
 
-// rows without a token among kZeroRows neighbours, from the sort's bits or
+// rows without a token among zero_rows neighbours, from the sort's bits or
 // else by a bisection a lane; neighbouring empty rows are cleared as one span
 __device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_t group) {
   const int lane = threadIdx.x & 63;
-  const int64_t row0 = group * kZeroRows, row = row0 + lane;
+  const int64_t row0 = group * a.zero_rows, row = row0 + lane;
+  const uint64_t within = (1ull << (a.V - row0 < a.zero_rows ? a.V - row0 : a.zero_rows)) - 1ull;
   uint64_t left;
   if (a.present) {
-    const uint32_t *words = a.present + rank * a.words + 2 * group;
-    const uint64_t there = (uint64_t)words[0] | (2 * group + 1 < a.words ? (uint64_t)words[1] << 32 : 0ull);
-    left = ~there & (a.V - row0 < 64 ? (1ull << (a.V - row0)) - 1ull : ~0ull);
+    left = ~(a.present[rank * a.words + row0 / 32] >> (row0 % 32)) & within;
   } else {
     const uint32_t *key = a.key + rank * a.T;
     int64_t lo = 0, hi = a.T;
@@ -575,15 +584,14 @@ __device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_
       if ((int64_t)key[mid] < row) lo = mid + 1;
       else hi = mid;
     }
-    left = __ballot(row < a.V && !(lo < a.T && (int64_t)key[lo] == row));
+    left = __ballot(!(lo < a.T && (int64_t)key[lo] == row)) & within;
   }
   float *base = a.grads + (rank * a.V + row0) * a.d;
   while (left) {
     const int s = __ffsll((unsigned long long)left) - 1;
-    const uint64_t gap = ~(left >> s);
-    const int len = gap ? __ffsll((unsigned long long)gap) - 1 : 64 - s;
+    const int len = __ffsll((unsigned long long)~(left >> s)) - 1;
     zero_span(base + (int64_t)s * a.d, (int64_t)len * a.d);
-    left &= len + s >= 64 ? 0ull : ~0ull << (s + len);
+    left &= ~0ull << (s + len);
   }
 }
 
@@ -665,70 +673,33 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
 }
 
 // Rows that cross a run's border: the run where such a row begins adds the
-// parts of the following runs, in order; of more than kJoinAlone parts the
-// workgroup's four waves add a quarter each, then the quarters' sums.
-constexpr int kJoinAlone = 8;
+// parts of the following runs.  A wave looks after one run; up to kJoinAlone
+// parts it adds itself, in order, longer rows are left to the whole workgroup,
+// a share of the parts a wave and then the shares' sums in order.  (A workgroup
+// for each run spent most of its 13 us at 65536 x 1536 on being launched.)
+constexpr int kJoinAlone = 8, kJoinWaves = 4;
 
-template <int VEC, bool ACC>
-__global__ __launch_bounds__(256) void embgrad_join_kernel(SumArgs a) {
-  __shared__ float quarter[4][64][VEC];
+// parts from .. to (exclusive) of a row, the p-th at part + p * stride, added to sum in order
+template <int VEC>
+__device__ __forceinline__ void add_parts(const float *part, int64_t stride, int64_t from, int64_t to, float sum[VEC]) {
   constexpr int kInFlight = 8;
-  const int64_t w = blockIdx.x;
-  const int64_t chunk = w % a.chunks, r = w / a.chunks, rank = r / a.runs, run = r - rank * a.runs;
-  const uint32_t *key = a.key + rank * a.T;
-  const int64_t lo = run * a.run, hi = lo + a.run;
-  if (hi >= a.T) return;
-  const uint32_t row = key[hi - 1];
-  if ((int64_t)row >= a.V || key[hi] != row) return;                     // nothing goes on
-  if (key[lo] == row && lo > 0 && key[lo - 1] == row) return;            // begun in an earlier run
-  // the runs behind this one that the row reaches: the end of its entries, by steps of a growing length, then bisection
-  int64_t b = hi, e = hi + a.run;
-  while (e < a.T && key[e] == row) {
-    b = e;
-    e += 2 * (e - hi);
-  }
-  e = e < a.T ? e : a.T;
-  while (b < e) {
-    const int64_t mid = (b + e) / 2;
-    if (key[mid] <= row) b = mid + 1;
-    else e = mid;
-  }
-  const int64_t last = (b - 1) / a.run, n = last - run;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const bool alone = n <= kJoinAlone;
-  if (alone && wave > 0) return;
-  const Columns<VEC> c(chunk, a.d);
-  const float *part = a.part + (rank * a.runs + run) * 2 * a.d4 + c.first;
-  const int64_t share = alone ? n : (n + 3) / 4;
-  const int64_t from = 1 + wave * share, to = from + share < n + 1 ? from + share : n + 1;
-  float sum[VEC];
+  for (int64_t u0 = from; u0 < to; u0 += kInFlight) {
+    float x[kInFlight][VEC];
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
-  if (c.any) {
-    if (wave == 0) load_row<VEC>(part + a.d4, sum);
-    for (int64_t u0 = from; u0 < to; u0 += kInFlight) {
-      float x[kInFlight][VEC];
+    for (int u = 0; u < kInFlight; ++u) load_row<VEC>(part + (u0 + u < to ? u0 + u : to - 1) * stride, x[u]);
+    __builtin_amdgcn_sched_barrier(0);      // all of them in flight before the first is added
 #pragma unroll
-      for (int u = 0; u < kInFlight; ++u) load_row<VEC>(part + (u0 + u < to ? u0 + u : to - 1) * 2 * a.d4, x[u]);
+    for (int u = 0; u < kInFlight; ++u) {
+      if (u0 + u >= to) break;
 #pragma unroll
-      for (int u = 0; u < kInFlight; ++u) {
-        if (u0 + u >= to) break;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) sum[k] += x[u][k];
-      }
+      for (int k = 0; k < VEC; ++k) sum[k] += x[u][k];
     }
   }
-  if (!alone) {
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) quarter[wave][lane][k] = sum[k];
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int q = 1; q < 4; ++q)
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) sum[k] += quarter[q][lane][k];
-  }
-  if (!c.any) return;
+}
+
+template <int VEC, bool ACC>
+__device__ __forceinline__ void finish_row(const SumArgs &a, int64_t rank, uint32_t row, const Columns<VEC> &c,
+                                           const float sum[VEC]) {
   float *p = a.grads + (rank * a.V + row) * a.d + c.first;
   float v[VEC], old[VEC];
   if constexpr (ACC) load_row<VEC>(p, old);
@@ -737,16 +708,87 @@ __global__ __launch_bounds__(256) void embgrad_join_kernel(SumArgs a) {
   keep_row<VEC>(p, c, v);
 }
 
+template <int VEC, bool ACC>
+__global__ __launch_bounds__(kJoinWaves * 64) void embgrad_join_kernel(SumArgs a) {
+  __shared__ float shares[kJoinWaves][64][VEC];
+  __shared__ int64_t parts[kJoinWaves];      // 0, or the parts of a row that is left to the workgroup
+  __shared__ uint32_t rows[kJoinWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  // workgroup: kJoinWaves runs of one rank and one chunk of columns
+  const int64_t groups = (a.runs + kJoinWaves - 1) / kJoinWaves;
+  const int64_t chunk = blockIdx.x % a.chunks, r = blockIdx.x / a.chunks, rank = r / groups;
+  const int64_t run0 = (r - rank * groups) * kJoinWaves, run = run0 + wave;
+  const uint32_t *key = a.key + rank * a.T;
+  const int64_t lo = run * a.run, hi = lo + a.run;
+  const Columns<VEC> c(chunk, a.d);
+  const float *part = a.part + (rank * a.runs + run) * 2 * a.d4 + c.first;
+  int64_t n = 0;
+  uint32_t row = 0;
+  if (hi < a.T) {
+    row = key[hi - 1];
+    const bool begun = key[lo] == row && lo > 0 && key[lo - 1] == row;
+    if ((int64_t)row < a.V && !begun) {
+      // the runs behind this one that begin with the row, 64 looked at together
+      for (bool more = true; more;) {
+        const int64_t i = (run + 1 + n + lane) * a.run;
+        const uint64_t there = __ballot(i < a.T && key[i < a.T ? i : 0] == row);
+        more = there == ~0ull;
+        n += more ? 64 : __ffsll((unsigned long long)~there) - 1;
+      }
+    }
+  }
+  if (lane == 0) {
+    parts[wave] = n > kJoinAlone ? n : 0;
+    rows[wave] = row;
+  }
+  if (n > 0 && n <= kJoinAlone && c.any) {
+    float sum[VEC];
+    load_row<VEC>(part + a.d4, sum);
+    add_parts<VEC>(part, 2 * a.d4, 1, n + 1, sum);
+    finish_row<VEC, ACC>(a, rank, row, c, sum);
+  }
+  __syncthreads();
+  for (int q = 0; q < kJoinWaves; ++q) {
+    const int64_t long_n = parts[q];
+    if (long_n == 0) continue;
+    const float *first = a.part + (rank * a.runs + run0 + q) * 2 * a.d4 + c.first;
+    const int64_t share = (long_n + kJoinWaves - 1) / kJoinWaves;
+    const int64_t from = 1 + wave * share, to = from + share < long_n + 1 ? from + share : long_n + 1;
+    float sum[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
+    if (c.any) {
+      if (wave == 0) load_row<VEC>(first + a.d4, sum);
+      add_parts<VEC>(first, 2 * a.d4, from, to, sum);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) shares[wave][lane][k] = sum[k];
+    __syncthreads();
+    if (wave == 0 && c.any) {
+#pragma unroll
+      for (int s = 1; s < kJoinWaves; ++s)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) sum[k] += shares[s][lane][k];
+      finish_row<VEC, ACC>(a, rank, rows[q], c, sum);
+    }
+    __syncthreads();
+  }
+}
+
 unsigned blocks_for(int64_t waves) { return (unsigned)((waves + 3) / 4); }
 
 // Elements of a lane: enough lanes of a wave at work on narrow rows, 16-byte
 // loads of bfloat16 on wide ones.
 int lane_columns(int64_t d) { return d > 256 ? 8 : d > 128 ? 4 : d > 64 ? 2 : 1; }
 
-int64_t column_chunks(int64_t d) {
-  const int64_t width = 64 * lane_columns(d);
-  return (d + width - 1) / width;
+// (an accumulating sum holds the old rows too: four columns take half the
+// registers, 65536 x 1536 103 -> 92 us)
+int sum_columns(int64_t d, bool accumulate) {
+  const int vec = lane_columns(d);
+  return accumulate && vec > 4 ? 4 : vec;
 }
+
+int64_t column_chunks(int64_t d, int vec) { return (d + 64 * vec - 1) / (64 * vec); }
 
 size_t a256(size_t b) { return (b + 255) & ~(size_t)255; }
 
@@ -754,8 +796,17 @@ size_t a256(size_t b) { return (b + 255) & ~(size_t)255; }
 // to 8 for short ranks, whose time is the longest chain of additions.
 int run_length(int64_t N, int64_t T, int64_t d) {
   int run = 32;
-  while (run > 8 && N * ((T + run - 1) / run) * column_chunks(d) < 2048) run /= 2;
+  while (run > 8 && N * ((T + run - 1) / run) * column_chunks(d, lane_columns(d)) < 2048) run /= 2;
   return run;
+}
+
+// Table rows that a wave looks over for empty ones: about 16 KB of them (8 x
+// 32000 x 1024: 64 rows a wave 202 us, 16 193, 8 and 4 183: neighbouring waves
+// then write neighbouring memory at the same time).
+int zero_rows_of(int64_t d) {
+  int rows = 4;
+  while (rows < 32 && rows * d < 4096) rows *= 2;
+  return rows;
 }
 
 struct GradPlan {
@@ -793,7 +844,7 @@ GradPlan grad_plan(int64_t N, int64_t T, int64_t V, int64_t d) {
 template <typename TIn, typename TOut>
 void lookup_launch(gift_ctx *ctx, const LookupJob &j) {
   const int vec = lane_columns(j.d);
-  const int chunks = (int)column_chunks(j.d);
+  const int chunks = (int)column_chunks(j.d, vec);
   const int rows = vec == 8 ? lookup_rows<TIn, 8>() : 4;
   const int64_t waves = (j.T + rows - 1) / rows * chunks;
   const dim3 grid(blocks_for(waves < 65536 * 4 ? waves : 65536 * 4));
@@ -815,14 +866,17 @@ gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
   hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC, ACC>), dim3(blocks_for(waves)), dim3(256), 0, ctx->stream, a);
   gift_status st = check_launch("embgrad_sum_kernel");
   if (st != GIFT_OK || a.runs < 2) return st;
-  hipLaunchKernelGGL((embgrad_join_kernel<VEC, ACC>), dim3((unsigned)a.run_waves), dim3(256), 0, ctx->stream, a);
+  const int64_t ranks = a.run_waves / (a.runs * a.chunks), groups = (a.runs + kJoinWaves - 1) / kJoinWaves;
+  hipLaunchKernelGGL((embgrad_join_kernel<VEC, ACC>), dim3((unsigned)(ranks * groups * a.chunks)),
+                     dim3(kJoinWaves * 64), 0, ctx->stream, a);
   return check_launch("embgrad_join_kernel");
 }
 
 template <typename TIn, bool ACC>
 gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
-  const int vec = lane_columns(a.d);
-  if (vec == 8) return sum_launch<TIn, 8, ACC>(ctx, a);
+  const int vec = sum_columns(a.d, ACC);
+  if constexpr (!ACC)
+    if (vec == 8) return sum_launch<TIn, 8, ACC>(ctx, a);
   if (vec == 4) return sum_launch<TIn, 4, ACC>(ctx, a);
   if (vec == 2) return sum_launch<TIn, 2, ACC>(ctx, a);
   return sum_launch<TIn, 1, ACC>(ctx, a);
@@ -902,9 +956,9 @@ size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d) {
 }
 
 int64_t embgrad_waves(const EmbGradJob &j) {
-  // a join takes a workgroup where the sum takes a wave
-  const int64_t run = (int64_t)j.N * ((j.T + run_length(j.N, j.T, j.d) - 1) / run_length(j.N, j.T, j.d)) * column_chunks(j.d);
-  return 4 * run + (j.accumulate ? 0 : (int64_t)j.N * ((j.V + kZeroRows - 1) / kZeroRows));
+  const int run = run_length(j.N, j.T, j.d);
+  return (int64_t)j.N * ((j.T + run - 1) / run + 3) * column_chunks(j.d, sum_columns(j.d, j.accumulate)) +
+         (j.accumulate ? 0 : (int64_t)j.N * ((j.V + zero_rows_of(j.d) - 1) / zero_rows_of(j.d)));
 }
 
 gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &j, char *ws) {
@@ -934,9 +988,10 @@ gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &j, char *ws) {
   a.words = p.words;
   a.run = p.run;
   a.runs = p.runs;
-  a.chunks = column_chunks(j.d);
+  a.chunks = column_chunks(j.d, sum_columns(j.d, j.accumulate));
   a.run_waves = (int64_t)j.N * p.runs * a.chunks;
-  a.zero_groups = (j.V + kZeroRows - 1) / kZeroRows;
+  a.zero_rows = zero_rows_of(j.d);
+  a.zero_groups = (j.V + a.zero_rows - 1) / a.zero_rows;
   a.zero_ranks = j.accumulate ? 0 : j.N;
   a.scale = j.scale;
   if (j.accumulate) return j.bf16 ? sum_launch<uint16_t, true>(ctx, a) : sum_launch<float, true>(ctx, a);
