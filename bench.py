@@ -30,6 +30,10 @@ the main stream, the others on further streams), and a GIFT matrix's encode
 waits only for its own group's refresh; the Euclidean matrices run beside the
 refresh.
 
+``--train-step f32|e4m3`` adds the training step around the codec: the
+embedding's gradient for every rank, and after the decode the gradient norm, the
+clipped AdamW step over all matrices and the embedding lookup.
+
 Prints one JSON line (metric: gradient GB/s through encode+decode; transform
 TFLOP/s; % of roofline).  ``--gpus N`` with N > 1 is not supported: this codec runs
 its N data-parallel ranks locally on one GPU.
@@ -141,6 +145,12 @@ def parse():
                     help="only measure the achievable peaks the roofline is compared with: the "
                          "library's float32 copy kernel over 1 GiB (HBM read + write) and matrix-core "
                          "loops with no memory traffic (bf16 16x16x32 and float32 16x16x4 MFMA)")
+    ap.add_argument("--train-step", choices=["none", "f32", "e4m3"], default="none",
+                    help="the training step around the codec, with the AdamW moments in float32 or "
+                         "E4M3: before the encode the embedding's rank gradients are formed from "
+                         "2048 tokens a rank (a set with an embedding; it then keeps a bucket of its "
+                         "own), after the decode follow the norm over all averaged gradients, the "
+                         "clipped AdamW step over all matrices and the next tokens' lookup")
     ap.add_argument("--copy-calibration", action="store_true",
                     help="only run the library's plain copy kernel on 256 MiB (5 launches), "
                          "the known-size reference for the HBM byte counters")
@@ -319,21 +329,24 @@ class Job:
 BUCKET_ELEMS = 1 << 26   # per rank: 256 MB of float32 gradient per bucket
 
 
-def buckets(wl, sides, gift, enable):
+def buckets(wl, sides, gift, enable, alone=()):
     """Matrices grouped into buckets of one shape, in step order.
 
     Euclidean matrices of one shape share buckets of up to BUCKET_ELEMS
     elements per rank; with the input-side transform alone the GIFT matrices
     that read the same layer input (gate, up) share a bucket, since their
-    common factor acts on rows independently; everything else is a bucket of
-    one.  Block rows must tile each matrix exactly."""
+    common factor acts on rows independently; everything else, and every
+    matrix named in `alone`, is a bucket of one.  Block rows must tile each
+    matrix exactly."""
     mats = wl.all_matrices()
     if not enable:
         return [[x] for x in mats]
     aligned = lambda mt: wl.block_rows == 0 or mt.m % wl.block_rows == 0
     out, open_eu = [], {}
     for layer, mt in mats:
-        if not mt.gift and aligned(mt):
+        if mt.name in alone:
+            out.append([(layer, mt)])
+        elif not mt.gift and aligned(mt):
             key = (mt.m, mt.n)
             b = open_eu.get(key)
             if b is None or (len(b) + 1) * mt.m * mt.n > BUCKET_ELEMS:
@@ -361,7 +374,7 @@ def build_workload(args, torch, gift, synth, dev):
         import dataclasses
         wl = dataclasses.replace(wl, name=wl.name + "-no-embedding", extra=())
     sides = gift.SIDE_INPUT if args.sides == "input" else gift.SIDE_BOTH
-    jobs = [Job(b, wl, sides, dev, torch, gift, args.format) for b in buckets(wl, sides, gift, args.bucket)]
+    jobs = [Job(b, wl, sides, dev, torch, gift, args.format) for b in buckets(wl, sides, gift, args.bucket, () if args.train_step == "none" else ("embed",))]
     # one random set per distinct shape, copied into every matrix's rows
     cache = {}
     for jb in jobs:
@@ -416,7 +429,54 @@ def build_workload(args, torch, gift, synth, dev):
 ctx_holder = {}
 
 
-def algorithmic_work(wl, jobs, args):
+class TrainStep:
+    """What a training program does around the codec: the embedding's rank
+    gradients from its tokens, and the clipped AdamW step on the averaged
+    gradients with the lookup that the next forward pass begins with."""
+
+    TOKENS = 2048       # per rank
+
+    def __init__(self, torch, gift, ctx, wl, jobs, moments, dev):
+        gen = torch.Generator(device=dev).manual_seed(77)
+        self.gift, self.jobs, self.moments = gift, jobs, moments
+        self.grads = [jb.out if jb.gift_branch else jb.mean for jb in jobs]
+        self.params = [torch.randn(g.shape, generator=gen, device=dev).mul_(0.02) for g in self.grads]
+        self.copies = [p.to(torch.bfloat16) for p in self.params]
+        self.norm = torch.empty(2, dtype=torch.float32, device=dev)
+        self.embed = next((i for i, jb in enumerate(jobs) if jb.mat.name == "embed"), None)
+        if self.embed is not None:
+            jb, T = jobs[self.embed], self.TOKENS
+            # Zipf's law over the vocabulary
+            u = torch.rand((wl.N, T), generator=gen, device=dev, dtype=torch.float64)
+            self.tokens = (torch.exp(u * torch.log(torch.tensor(jb.m + 1.0))) - 1).long().clamp_(0, jb.m - 1)
+            self.dout = torch.randn((wl.N, T, jb.n), generator=gen, device=dev).mul_(2.15e-4).to(torch.bfloat16)
+            self.rows = torch.empty((wl.N, T, jb.n), dtype=torch.bfloat16, device=dev)
+        self.opt = gift.AdamW(ctx, self.params, weight_decay=0.1, moments=moments, copies=self.copies)
+
+    def before(self, ctx, jb):
+        """The embedding's rank gradients, before its encode on the same stream."""
+        if self.embed is not None and jb is self.jobs[self.embed]:
+            self.gift.embedding_grad(ctx, self.tokens, self.dout, jb.grads)
+
+    def after(self, ctx):
+        """Norm, step and lookup, once every averaged gradient is there."""
+        self.gift.grad_norm(ctx, self.grads, self.norm, max_norm=1.0)
+        self.opt.step(self.grads, lr=3e-4, grad_scale=self.norm[1:])
+        if self.embed is not None:
+            self.gift.embedding(ctx, self.copies[self.embed], self.tokens, self.rows)
+
+    def work(self):
+        """(family, flops, bytes) of one step."""
+        e = float(sum(p.numel() for p in self.params))
+        out = [("norm", 2 * e, 4 * e),
+               ("optimizer", 16 * e, e * (14 + (16 if self.moments == "f32" else 4 + 16 / 256)))]
+        if self.embed is not None:
+            t, (V, d) = float(self.dout.numel()), self.params[self.embed].shape
+            out += [("embed_grad", t, 2 * t + 4.0 * self.tokens.shape[0] * V * d), ("embed", 0.0, 4 * t)]
+        return out
+
+
+def algorithmic_work(wl, jobs, args, train=None):
     """Algorithmic flops / bytes per step for each kernel family."""
     r = wl.rank
     fam = {}
@@ -476,6 +536,8 @@ def algorithmic_work(wl, jobs, args):
             add("factor", refresh * sub, 0)
             # the k x k Cholesky factorisations and the eigensolver are
             # latency-bound single-workgroup kernels: timed, no roofline
+    for name, flops, bytes_ in (train.work() if train else ()):
+        add(name, flops, bytes_)
     return fam
 
 
@@ -731,6 +793,7 @@ def main():
           f"{sum(j.N * j.m * j.n for j in jobs) * 4 / 1e9:.2f} GB of rank gradients", file=sys.stderr,
           flush=True)
 
+    train = TrainStep(torch, gift, ctx, wl, jobs, args.train_step, dev) if args.train_step != "none" else None
     fjobs = [jb for jb in jobs if jb.owns_factor]
     # independent matrices on several streams (default priority), one library
     # context per stream.  The factor refresh runs per factor shape (one call
@@ -831,6 +894,8 @@ def main():
                     streams[sid].wait_event(ev)    # GIFT encodes need the refreshed factor
                     waited.add((sid, jb.group))
             c = ctxs[sid]
+            if train:
+                train.before(c, jb)
             if args.format == "mxfp4":
                 gift.encode_mxfp4(c, jb.factor, jb.grads, jb.codes, jb.scales, ef=jb.ef)
                 gift.reduce_local_mxfp4(c, jb.codes, jb.scales, jb.mean)
@@ -849,6 +914,9 @@ def main():
         for (sid, _, _), jbs in pending.items():
             gift.decode_batch(ctxs[sid], [jb.factor for jb in jbs], [jb.mean for jb in jbs],
                               [jb.out for jb in jbs])
+        if train and codec:
+            join_into_main()
+            train.after(ctx)
 
     for w in range(max(args.warmup, 1)):
         step(args.cold_iters if w == 0 else args.iters)
@@ -894,7 +962,7 @@ def main():
     # the dominant kernel: the family with the most time per step among
     # those with a roofline (algorithmic bytes or flops); the refresh's
     # one-workgroup-per-factor k x k kernels (chol, eig) are latency-bound
-    work = algorithmic_work(wl, jobs, args)
+    work = algorithmic_work(wl, jobs, args, train)
     with_roof = [k for k in fam_ms if sum(work.get(k, (0.0, 0.0))) > 0]
     dom = max(with_roof or list(fam_ms), key=lambda k: fam_ms[k][1])
     latency_ms = {k: round(fam_ms[k][1], 4) for k in fam_ms if k not in with_roof}
@@ -1025,6 +1093,8 @@ def main():
                         "pass with every launch on one stream",
         "latency_bound_ms_per_step": latency_ms,
     }
+    if train:
+        line["config"]["train_step"] = args.train_step
     if not args.no_cpu_baseline:
         print("[bench] timing the oracle on the host", file=sys.stderr, flush=True)
         line["cpu_baseline"] = cpu_baseline(wl, jobs, args.cpu_seconds)
