@@ -42,9 +42,10 @@ __device__ __forceinline__ int find_tensor(const uint32_t *first, int count, uin
 // ---------------------------------------------------------------------------
 // Squares and sums in float64: no overflow of a square, and the result does
 // not depend on how the elements are spread over the workgroups beyond its
-// last bits.  Bound by reading the gradients once.
+// last bits.  Bound by reading the gradients once: past the caches, 374 M
+// float32 elements in 224 us, 6.7 TB/s (through them 247 us).
 constexpr int kNormTensors = 128;
-constexpr int kNormChunk = 8192;      // elements of a workgroup's step
+constexpr int kNormChunk = 4096;      // elements of a workgroup's step
 constexpr int kNormGroups = 2048;     // workgroups, one partial sum each
 
 struct NormArgs {
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
       const uint16_t *p = static_cast<const uint16_t *>(a.ptr[t]) + at;
       const int vec = (reinterpret_cast<uintptr_t>(p) & 15) == 0 ? n / 8 : 0;
       for (int i = threadIdx.x; i < vec; i += 256) {
-        const uintx4 x = reinterpret_cast<const uintx4 *>(p)[i];
+        const uintx4 x = __builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(p) + i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) add_square(acc[k], bf16_lo(x[k])), add_square(acc[k], bf16_hi(x[k]));
       }
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
       const float *p = static_cast<const float *>(a.ptr[t]) + at;
       const int vec = (reinterpret_cast<uintptr_t>(p) & 15) == 0 ? n / 4 : 0;
       for (int i = threadIdx.x; i < vec; i += 256) {
-        const floatx4 x = reinterpret_cast<const floatx4 *>(p)[i];
+        const floatx4 x = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(p) + i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) add_square(acc[k], x[k]);
       }

@@ -543,28 +543,30 @@ def decode_batch(ctx: Context, factors, means, outs):
 # ---------------------------------------------------------------------------
 # The training step around the codec
 # ---------------------------------------------------------------------------
+# (small calls take less time on the GPU than in Python: torch is a module
+# global here, it was imported before the library)
+import torch  # noqa: E402
+
+_VALUES = {torch.float32: F32, torch.bfloat16: BF16}
+_INDICES = {torch.int32: I32, torch.int64: I64}
+
 
 def _value_dtype(t, name):
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    dt = _VALUES.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return dt
 
 
 def _index_type(t, name):
-    import torch
-    if t.dtype == torch.int32:
-        return I32
-    if t.dtype == torch.int64:
-        return I64
-    raise TypeError(f"{name} must be int32 or int64, not {t.dtype}")
+    it = _INDICES.get(t.dtype)
+    if it is None:
+        raise TypeError(f"{name} must be int32 or int64, not {t.dtype}")
+    return it
 
 
 def _on_current_device(**tensors):
     """Raise ValueError unless every tensor is contiguous and on the current device."""
-    import torch
     dev = None
     for name, t in tensors.items():
         at = t.get_device()
@@ -583,17 +585,18 @@ def _scratch(t):
     if t is None:
         return None, 0
     _on_current_device(scratch=t)
-    return ctypes.c_void_p(t.data_ptr()), t.numel() * t.element_size()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def embedding(ctx: Context, table, tokens, out, scale: float = 1.0):
     """``gift_embedding``: ``out[...] = scale * table[tokens[...]]``; table [V, d] and out
     [*tokens.shape, d] float32 or bfloat16, tokens int32 or int64 (ids outside [0, V): zeros)."""
     V, d = _dims(table, 2, "table")
-    _expect(out, tuple(tokens.shape) + (d,), "out")
+    if out.shape != tokens.shape + (d,):
+        _expect(out, tuple(tokens.shape) + (d,), "out")
     td, it, od = _value_dtype(table, "table"), _index_type(tokens, "tokens"), _value_dtype(out, "out")
     _on_current_device(table=table, tokens=tokens, out=out)
-    _check(LIB.gift_embedding(ctx.handle, table.data_ptr(), td, V, d, tokens.data_ptr(), it, tokens.numel(), scale,
+    _check(LIB.gift_embedding(ctx._h, table.data_ptr(), td, V, d, tokens.data_ptr(), it, tokens.numel(), scale,
                               out.data_ptr(), od))
 
 
@@ -608,7 +611,6 @@ def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumu
     added to what grads holds.  ``scratch``: a tensor of at least
     :func:`embedding_grad_scratch` bytes (needed under graph capture), else the
     context's workspace."""
-    import torch
     N, V, d = _dims(grads, 3, "grads")
     T = _dims(tokens, 2, "tokens")[1]
     _expect(tokens, (N, T), "tokens")
@@ -618,7 +620,7 @@ def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumu
         raise TypeError(f"grads must have dtype torch.float32, not {grads.dtype}")
     _on_current_device(tokens=tokens, dout=dout, grads=grads)
     ws, ws_bytes = _scratch(scratch)
-    _check(LIB.gift_embedding_grad(ctx.handle, tokens.data_ptr(), it, dout.data_ptr(), dt, N, T, V, d, scale,
+    _check(LIB.gift_embedding_grad(ctx._h, tokens.data_ptr(), it, dout.data_ptr(), dt, N, T, V, d, scale,
                                    1 if accumulate else 0, grads.data_ptr(), ws, ws_bytes))
 
 
@@ -630,7 +632,6 @@ def _gradient_list(grads):
 
     Loops of C functions: a model has hundreds of tensors, and a step's kernels
     take less time than hundreds of passes through Python."""
-    import torch
     T = torch.Tensor
     dt = _value_dtype(grads[0], "gradients")
     if len(set(map(_DTYPE, grads))) > 1:
@@ -651,7 +652,6 @@ def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=
     (NaN when the norm is not finite).  ``scratch``: a tensor of at least
     ``GRAD_NORM_SCRATCH_BYTES`` bytes (needed under graph capture), else the
     context's workspace."""
-    import torch
     grads = list(grads)
     _expect(out, (2,), "out")
     if out.dtype != torch.float32:
@@ -661,7 +661,7 @@ def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=
     dt, ptrs = _gradient_list(grads) if count else (F32, array.array("Q"))
     sizes = array.array("q", map(torch.Tensor.numel, grads))
     ws, ws_bytes = _scratch(scratch)
-    _check(LIB.gift_grad_norm(ctx.handle, count, ptrs.buffer_info()[0], sizes.buffer_info()[0], dt, max_norm,
+    _check(LIB.gift_grad_norm(ctx._h, count, ptrs.buffer_info()[0], sizes.buffer_info()[0], dt, max_norm,
                               out.data_ptr(), ws, ws_bytes))
 
 
@@ -681,7 +681,6 @@ class AdamW:
 
     def __init__(self, ctx: Context, params, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0,
                  moments: str = "f32", seed: int = 0, state=None, copies=None):
-        import torch
         if moments not in MOMENTS:
             raise ValueError(f"moments must be one of {sorted(MOMENTS)}, not {moments!r}")
         self.ctx, self.params, self.betas, self.eps, self.moments = ctx, list(params), betas, eps, moments
@@ -752,7 +751,6 @@ class AdamW:
     @classmethod
     def state_sizes(cls, params, moments: str = "f32"):
         """``{name: (elements, dtype)}`` of the flat state tensors."""
-        import torch
         total = cls._starts(params)[1]
         if moments == "f32":
             return {"m": (total, torch.float32), "v": (total, torch.float32)}
@@ -768,7 +766,6 @@ class AdamW:
         both as tensors where they change from replay to replay.
         ``grad_scale``: a float32 tensor of one element; NaN skips the step.
         """
-        import torch
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError("grads must have one entry per parameter")
@@ -795,6 +792,6 @@ class AdamW:
         if grads:
             o.grad_dtype, ptrs = _gradient_list(grads)
             self._grad_words[:] = memoryview(ptrs)
-        _check(LIB.gift_adamw_step(self.ctx.handle, len(grads), self._tensors, ctypes.byref(o)))
+        _check(LIB.gift_adamw_step(self.ctx._h, len(grads), self._tensors, ctypes.byref(o)))
         if not on_device:
             self.steps = number
