@@ -431,9 +431,9 @@ struct EmbGradJob {
   bool bf16 = false, wide = false, accumulate = false;
 };
 size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d);
-// the waves of its largest launch; one launch takes up to kMaxWaves
-int64_t embgrad_waves(const EmbGradJob &job);
-constexpr int64_t kMaxWaves = (1LL << 26) - 4;   // 2^32 threads of a grid dimension
+// the workgroups of its largest launch; one launch takes up to kMaxBlocks of 256 threads
+int64_t embgrad_blocks(const EmbGradJob &job);
+constexpr int64_t kMaxBlocks = (1LL << 24) - 1;   // a grid dimension has fewer than 2^32 threads
 gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &job, char *ws);
 
 size_t grad_norm_scratch();

@@ -130,7 +130,7 @@ gift_status gift_embedding_grad(gift_ctx *ctx, const void *tokens, gift_index_ty
   j.wide = token_type == GIFT_I64;
   j.accumulate = accumulate != 0;
   if (T == 0 && accumulate) return GIFT_OK;
-  if (embgrad_waves(j) > kMaxWaves) return fail(GIFT_ESHAPE, call, "more work than one launch takes");
+  if (embgrad_blocks(j) > kMaxBlocks) return fail(GIFT_ESHAPE, call, "more work than one launch takes");
   if ((st = enter(ctx, call)) != GIFT_OK) return st;
   void *ws = nullptr;
   if (T > 0 && (st = take_scratch(ctx, call, scratch, scratch_bytes, embgrad_scratch(N, T, V, d), 256, &ws)) != GIFT_OK)

@@ -17,6 +17,7 @@
 // behind all others and nothing reads them.
 
 #include "gift_internal.h"
+#include "xcd_map.h"
 
 namespace gift {
 
@@ -38,39 +39,50 @@ __device__ __forceinline__ uint32_t to_bf16(float x) {
   return x != x ? (u >> 16 | 0x40u) : (u + 0x7fffu + (u >> 16 & 1u)) >> 16;
 }
 
-// VEC neighbouring elements of a row as float32
-template <int VEC>
-__device__ __forceinline__ void load_row(const float *p, float v[VEC]) {
-  if constexpr (VEC >= 4) {
-#pragma unroll
-    for (int i = 0; i < VEC; i += 4) {
-      const floatx4_u x = *reinterpret_cast<const floatx4_u *>(p + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[i + k] = x[k];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = p[i];
-  }
-}
+// VEC neighbouring elements of a row as loaded: converted only where they are
+// used, so that several rows' loads are in flight together.
+template <typename T, int VEC>
+struct RowBits;
 
 template <int VEC>
-__device__ __forceinline__ void load_row(const uint16_t *p, float v[VEC]) {
-  if constexpr (VEC == 8) {
-    const uintx4_u x = *reinterpret_cast<const uintx4_u *>(p);
+struct RowBits<float, VEC> {
+  float x[VEC];
+  __device__ __forceinline__ void load(const float *p) {
+    if constexpr (VEC >= 4) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[2 * k] = bf16_lo(x[k]), v[2 * k + 1] = bf16_hi(x[k]);
-  } else if constexpr (VEC == 4) {
-    const uintx2_u x = *reinterpret_cast<const uintx2_u *>(p);
+      for (int i = 0; i < VEC; i += 4) {
+        const floatx4_u w = *reinterpret_cast<const floatx4_u *>(p + i);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) v[2 * k] = bf16_lo(x[k]), v[2 * k + 1] = bf16_hi(x[k]);
-  } else if constexpr (VEC == 2) {
-    const uint32_t x = *reinterpret_cast<const uintx1_u *>(p);
-    v[0] = bf16_lo(x), v[1] = bf16_hi(x);
-  } else {
-    v[0] = bf16_lo(p[0]);
+        for (int k = 0; k < 4; ++k) x[i + k] = w[k];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = p[i];
+    }
   }
-}
+  __device__ __forceinline__ float operator[](int k) const { return x[k]; }
+};
+
+template <int VEC>
+struct RowBits<uint16_t, VEC> {
+  uint32_t w[(VEC + 1) / 2];
+  __device__ __forceinline__ void load(const uint16_t *p) {
+    if constexpr (VEC == 8) {
+      const uintx4_u x = *reinterpret_cast<const uintx4_u *>(p);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = x[k];
+    } else if constexpr (VEC == 4) {
+      const uintx2_u x = *reinterpret_cast<const uintx2_u *>(p);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) w[k] = x[k];
+    } else if constexpr (VEC == 2) {
+      w[0] = *reinterpret_cast<const uintx1_u *>(p);
+    } else {
+      w[0] = p[0];
+    }
+  }
+  __device__ __forceinline__ float operator[](int k) const { return k & 1 ? bf16_hi(w[k / 2]) : bf16_lo(w[k / 2]); }
+};
 
 template <int VEC>
 __device__ __forceinline__ void store_row(float *p, const float v[VEC]) {
@@ -126,20 +138,19 @@ __device__ __forceinline__ void stream_row(uint16_t *p, const float v[VEC]) {
   }
 }
 
-// Columns of a lane: VEC from `first` on.  The row's last lane holds fewer:
-// it loads the VEC columns that end the row and keeps the last `own` of them.
+// Columns of a lane: VEC from `first` on, always inside the row.  The row's last
+// lane holds fewer: it loads the VEC columns that end the row, and the first
+// `skip` of them belong to the lane before; lanes behind it load the same ones
+// and own none (skip >= VEC).
 template <int VEC>
 struct Columns {
-  int64_t first;   // first column loaded
-  int skip;        // of these, columns that belong to the lane before
-  bool any;
+  int64_t first, skip;
   __device__ __forceinline__ Columns(int64_t chunk, int64_t d) {
-    const int64_t c = (chunk * 64 + (threadIdx.x & 63)) * VEC;
-    any = c < d;
-    const int64_t last = d - VEC;
+    const int64_t c = (chunk * 64 + (threadIdx.x & 63)) * VEC, last = d - VEC;
     first = c <= last ? c : last;
-    skip = (int)(c - first);
+    skip = c - first;
   }
+  __device__ __forceinline__ bool any() const { return skip < VEC; }
 };
 
 __device__ __forceinline__ int64_t read_token(const void *tokens, bool wide, int64_t i) {
@@ -168,24 +179,25 @@ __global__ __launch_bounds__(256) void lookup_kernel(const TIn *table, const voi
   for (int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); i < items; i += stride) {
     const int64_t group = i / chunks, t0 = group * kLookupRows;
     const Columns<VEC> c(i - group * chunks, d);
-    if (!c.any) continue;
-    float v[kLookupRows][VEC];
+    if (!c.any()) continue;
+    RowBits<TIn, VEC> x[kLookupRows];
     bool in[kLookupRows];
 #pragma unroll
     for (int r = 0; r < kLookupRows; ++r) {
       const int64_t id = read_token(tokens, wide, t0 + r < T ? t0 + r : T - 1);
       in[r] = id >= 0 && id < V;
-      load_row<VEC>(table + (in[r] ? id : 0) * d + c.first, v[r]);
+      x[r].load(table + (in[r] ? id : 0) * d + c.first);
     }
 #pragma unroll
     for (int r = 0; r < kLookupRows; ++r) {
       if (t0 + r >= T) break;
+      float v[VEC];
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) v[r][k] = in[r] ? v[r][k] * scale : 0.f;
+      for (int k = 0; k < VEC; ++k) v[k] = in[r] ? x[r][k] * scale : 0.f;
       // (a row's last lane rewrites columns of the one before with the same values)
       TOut *p = out + (t0 + r) * d + c.first;
-      if constexpr (STREAM) stream_row<VEC>(p, v[r]);
-      else store_row<VEC>(p, v[r]);
+      if constexpr (STREAM) stream_row<VEC>(p, v);
+      else store_row<VEC>(p, v);
     }
   }
 }
@@ -352,8 +364,7 @@ struct SortArgs {
   const uint32_t *key_in, *pos_in;
   uint32_t *key_out, *pos_out;
   uint32_t *hist;          // [N][tiles][256] counts, then first places
-  uint32_t *present;       // null, or [N][words] (LdsSortArgs): cleared by the first pass, set by the second
-  int64_t T, V, words;
+  int64_t T, V;
   int tiles, shift;
 };
 
@@ -366,10 +377,6 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t rank, in
 __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(SortArgs a) {
   __shared__ uint32_t count[kDigits];
   const int64_t rank = blockIdx.y;
-  uint32_t *present = a.present ? a.present + rank * a.words : nullptr;
-  if (present && a.shift == 0)
-    for (int64_t w = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; w < a.words; w += (int64_t)gridDim.x * kSortThreads)
-      present[w] = 0;
   count[threadIdx.x] = 0;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * kSortTile + threadIdx.x;
@@ -379,12 +386,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(SortArgs a) {
     key[it] = lo + it * kSortThreads < a.T ? sort_key(a, rank, lo + it * kSortThreads) : 0xffffffffu;
 #pragma unroll
   for (int it = 0; it < kSortItems; ++it) {
-    const uint32_t k = key[it];
-    if (lo + it * kSortThreads >= a.T) continue;
-    atomicAdd(&count[(k >> a.shift) & 255u], 1u);
-    // (a bit already seen as set need not be set again: frequent tokens)
-    if (present && a.shift == 8 && (int64_t)k < a.V && !(present[k / 32] >> (k % 32) & 1u))
-      atomicOr(&present[k / 32], 1u << (k % 32));
+    if (lo + it * kSortThreads < a.T) atomicAdd(&count[(key[it] >> a.shift) & 255u], 1u);
   }
   __syncthreads();
   a.hist[(rank * a.tiles + blockIdx.x) * kDigits + threadIdx.x] = count[threadIdx.x];
@@ -536,9 +538,10 @@ struct SumArgs {
   const uint32_t *present;     // null, or [N][words] (LdsSortArgs)
   int64_t T, V, d, d4, words;
   int64_t runs, chunks, run_waves;
-  int64_t zero_groups, zero_ranks;   // waves behind run_waves: zero_ranks x zero_groups
+  int64_t zero_groups, zero_ranks;   // groups of zero_rows table rows of a rank; ranks to look over
+  int64_t run_blocks;                // workgroups of the runs, a multiple of 8; one a zero group follows
   int run;                           // ordered entries of one wave, at most 64
-  int zero_rows;                     // table rows looked over by one wave, a power of two up to 32
+  int zero_rows;                     // table rows looked over by one workgroup, a power of two up to 32
   float scale;
 };
 
@@ -554,41 +557,44 @@ __device__ __forceinline__ void keep_row(float *p, const Columns<VEC> &c, const 
   }
 }
 
-// n consecutive floats set to zero by one wave: whole 128-byte lines past the
-// caches, what is left at either end through them (streamed parts of lines
-// cost their whole line: 3 x 50001 rows of 771 109 us, now 95)
+// n consecutive floats set to zero by one workgroup: whole 128-byte lines past
+// the caches, what is left at either end through them (streamed parts of lines
+// cost their whole line)
 __device__ __forceinline__ void zero_span(float *p, int64_t n) {
-  const int lane = threadIdx.x & 63;
   const int64_t lead = (-(int64_t)(reinterpret_cast<uintptr_t>(p) / 4)) & 31, skip = lead < n ? lead : n;
-  if (lane < skip) p[lane] = 0.f;
+  if (threadIdx.x < skip) p[threadIdx.x] = 0.f;       // up to a line of 128 bytes
   p += skip;
   n -= skip;
   const int64_t whole = n & ~31ll;
-  for (int64_t i = lane * 4; i < whole; i += 256)
+  for (int64_t i = threadIdx.x * 4; i < whole; i += 1024)
     __builtin_nontemporal_store(floatx4_u{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<floatx4_u *>(p + i));
-  if (lane < n - whole) p[whole + lane] = 0.f;
+  if (threadIdx.x < n - whole) p[whole + threadIdx.x] = 0.f;
 }
 
-// rows without a token among zero_rows neighbours, from the sort's bits or
-// else by a bisection a lane; neighbouring empty rows are cleared as one span
-__device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_t group) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row0 = group * a.zero_rows, row = row0 + lane;
-  const uint64_t within = (1ull << (a.V - row0 < a.zero_rows ? a.V - row0 : a.zero_rows)) - 1ull;
-  uint64_t left;
-  if (a.present) {
-    left = ~(a.present[rank * a.words + row0 / 32] >> (row0 % 32)) & within;
-  } else {
-    const uint32_t *key = a.key + rank * a.T;
-    int64_t lo = 0, hi = a.T;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if ((int64_t)key[mid] < row) lo = mid + 1;
-      else hi = mid;
-    }
-    left = __ballot(!(lo < a.T && (int64_t)key[lo] == row)) & within;
+// Bits of the neighbouring rows from row0 on that occur among a rank's T ordered
+// keys, by a bisection a lane (a search by the whole wave, 64 keys at a time,
+// starts again behind every frequent token: 131072 positions 62 -> 116 us).
+__device__ __forceinline__ uint64_t rows_there(const uint32_t *key, int64_t T, int64_t row0) {
+  const int64_t row = row0 + (threadIdx.x & 63);
+  int64_t lo = 0, hi = T;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if ((int64_t)key[mid] < row) lo = mid + 1;
+    else hi = mid;
   }
+  return __ballot(lo < T && (int64_t)key[lo] == row);
+}
+
+// Rows without a token among zero_rows neighbours, from the sort's bits or else
+// by bisection (every wave of the workgroup for itself); neighbouring empty rows
+// are cleared as one span.
+__device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t rank, int64_t group) {
+  const int64_t row0 = group * a.zero_rows;
+  const int rows = (int)(a.V - row0 < a.zero_rows ? a.V - row0 : a.zero_rows);
+  const uint64_t there = a.present ? a.present[rank * a.words + row0 / 32] >> (row0 % 32)
+                                   : rows_there(a.key + rank * a.T, a.T, row0);
   float *base = a.grads + (rank * a.V + row0) * a.d;
+  uint64_t left = ~there & ((1ull << rows) - 1ull);
   while (left) {
     const int s = __ffsll((unsigned long long)left) - 1;
     const int len = __ffsll((unsigned long long)~(left >> s)) - 1;
@@ -602,13 +608,13 @@ template <typename TIn, int VEC, bool ACC>
 __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
   constexpr int kInFlight = ACC ? 4 : 8;      // rows loaded ahead
   const int lane = threadIdx.x & 63;
-  int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if (w >= a.run_waves) {
-    w -= a.run_waves;
-    const int64_t rank = w / a.zero_groups;
-    if (rank < a.zero_ranks) zero_rows(a, rank, w - rank * a.zero_groups);
+  if ((int64_t)blockIdx.x >= a.run_blocks) {
+    const int64_t g = xcd_tile((int64_t)blockIdx.x - a.run_blocks, a.zero_ranks * a.zero_groups), rank = g / a.zero_groups;
+    zero_rows(a, rank, g - rank * a.zero_groups);
     return;
   }
+  const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if (w >= a.run_waves) return;
   const int64_t chunk = w % a.chunks, r = w / a.chunks, rank = r / a.runs, run = r - rank * a.runs;
   const uint32_t *key = a.key + rank * a.T, *pos = a.pos + rank * a.T;
   const int64_t lo = run * a.run, hi = lo + a.run < a.T ? lo + a.run : a.T;
@@ -628,7 +634,6 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
   const bool goes_on = count == hi - lo && key_behind == (uint32_t)__builtin_amdgcn_readlane(my_key, count - 1);
   float sum[VEC], old[VEC];
   auto flush = [&](bool tail) {
-    if (!c.any) return;
     if (head || tail) {
       keep_row<VEC>(part + (head ? 0 : a.d4), c, sum);
       return;
@@ -639,7 +644,8 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
     keep_row<VEC>(grads + (int64_t)row * a.d, c, v);
   };
   for (int i0 = 0; i0 < count; i0 += kInFlight) {
-    float x[kInFlight][VEC], was[ACC ? kInFlight : 1][VEC];
+    RowBits<TIn, VEC> x[kInFlight];
+    RowBits<float, VEC> was[ACC ? kInFlight : 1];
     uint32_t k[kInFlight];
     bool starts[kInFlight];
 #pragma unroll
@@ -648,10 +654,11 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
       k[u] = (uint32_t)__builtin_amdgcn_readlane(my_key, i);
       starts[u] = i0 + u < count && (i == 0 || k[u] != (uint32_t)__builtin_amdgcn_readlane(my_key, i > 0 ? i - 1 : 0));
       const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(my_pos, i);
-      if (c.any) load_row<VEC>(dout + (int64_t)p * a.d, x[u]);
+      x[u].load(dout + (int64_t)p * a.d);
       if constexpr (ACC)
-        if (starts[u] && c.any) load_row<VEC>(grads + (int64_t)k[u] * a.d, was[u]);
+        if (starts[u]) was[u].load(grads + (int64_t)k[u] * a.d);
     }
+    __builtin_amdgcn_sched_barrier(0);      // all of them in flight before the first is added
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (i0 + u >= count) break;
@@ -681,14 +688,22 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
 // for each run spent most of its 13 us at 65536 x 1536 on being launched.)
 constexpr int kJoinAlone = 8, kJoinWaves = 4;
 
+template <int VEC>
+__device__ __forceinline__ void load_sum(const float *p, float sum[VEC]) {
+  RowBits<float, VEC> x;
+  x.load(p);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) sum[k] = x[k];
+}
+
 // parts from .. to (exclusive) of a row, the p-th at part + p * stride, added to sum in order
 template <int VEC>
 __device__ __forceinline__ void add_parts(const float *part, int64_t stride, int64_t from, int64_t to, float sum[VEC]) {
   constexpr int kInFlight = 8;
   for (int64_t u0 = from; u0 < to; u0 += kInFlight) {
-    float x[kInFlight][VEC];
+    RowBits<float, VEC> x[kInFlight];
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) load_row<VEC>(part + (u0 + u < to ? u0 + u : to - 1) * stride, x[u]);
+    for (int u = 0; u < kInFlight; ++u) x[u].load(part + (u0 + u < to ? u0 + u : to - 1) * stride);
     __builtin_amdgcn_sched_barrier(0);      // all of them in flight before the first is added
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
@@ -703,8 +718,9 @@ template <int VEC, bool ACC>
 __device__ __forceinline__ void finish_row(const SumArgs &a, int64_t rank, uint32_t row, const Columns<VEC> &c,
                                            const float sum[VEC]) {
   float *p = a.grads + (rank * a.V + row) * a.d + c.first;
-  float v[VEC], old[VEC];
-  if constexpr (ACC) load_row<VEC>(p, old);
+  float v[VEC];
+  RowBits<float, VEC> old;
+  if constexpr (ACC) old.load(p);
 #pragma unroll
   for (int k = 0; k < VEC; ++k) v[k] = ACC ? old[k] + sum[k] * a.scale : sum[k] * a.scale;
   keep_row<VEC>(p, c, v);
@@ -743,9 +759,9 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embgrad_join_kernel(SumArgs a
     parts[wave] = n > kJoinAlone ? n : 0;
     rows[wave] = row;
   }
-  if (n > 0 && n <= kJoinAlone && c.any) {
+  if (n > 0 && n <= kJoinAlone) {
     float sum[VEC];
-    load_row<VEC>(part + a.d4, sum);
+    load_sum<VEC>(part + a.d4, sum);
     add_parts<VEC>(part, 2 * a.d4, 1, n + 1, sum);
     finish_row<VEC, ACC>(a, rank, row, c, sum);
   }
@@ -759,14 +775,12 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embgrad_join_kernel(SumArgs a
     float sum[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
-    if (c.any) {
-      if (wave == 0) load_row<VEC>(first + a.d4, sum);
-      add_parts<VEC>(first, 2 * a.d4, from, to, sum);
-    }
+    if (wave == 0) load_sum<VEC>(first + a.d4, sum);
+    add_parts<VEC>(first, 2 * a.d4, from, to, sum);
 #pragma unroll
     for (int k = 0; k < VEC; ++k) shares[wave][lane][k] = sum[k];
     __syncthreads();
-    if (wave == 0 && c.any) {
+    if (wave == 0) {
 #pragma unroll
       for (int s = 1; s < kJoinWaves; ++s)
 #pragma unroll
@@ -802,9 +816,7 @@ int run_length(int64_t N, int64_t T, int64_t d) {
   return run;
 }
 
-// Table rows that a wave looks over for empty ones: about 16 KB of them (8 x
-// 32000 x 1024: 64 rows a wave 202 us, 16 193, 8 and 4 183: neighbouring waves
-// then write neighbouring memory at the same time).
+// Table rows that a workgroup looks over for empty ones: about 16 KB.
 int zero_rows_of(int64_t d) {
   int rows = 4;
   while (rows < 32 && rows * d < 4096) rows *= 2;
@@ -823,9 +835,10 @@ GradPlan grad_plan(int64_t N, int64_t T, int64_t V, int64_t d) {
   p.runs = (T + p.run - 1) / p.run;
   p.d4 = (d + 3) / 4 * 4;
   p.tiles = T <= kLdsKeys ? 0 : (int)((T + kSortTile - 1) / kSortTile);
-  // (past 2^20 rows the windows of the sort in LDS would take longer than the
-  // bisections; a sort of one pass has no second one that sets them)
-  p.words = V <= 1 << 20 && (V >= 256 || p.tiles == 0) ? (V + 31) / 32 : 0;
+  // row bits from the sort in LDS (past 2^20 rows its windows would take longer
+  // than the bisections; the sort through memory leaves none: set there by
+  // atomics, frequent tokens' words took 180 us at 65536 positions)
+  p.words = p.tiles == 0 && V <= 1 << 20 ? (V + 31) / 32 : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -876,8 +889,13 @@ void lookup_launch(gift_ctx *ctx, const LookupJob &j) {
 
 template <typename TIn, int VEC, bool ACC>
 gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
-  const int64_t waves = a.run_waves + a.zero_ranks * a.zero_groups;
-  hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC, ACC>), dim3(blocks_for(waves)), dim3(256), 0, ctx->stream, a);
+  // How fast memory takes the zeros hangs on how much of it is written at the
+  // same time: 8 x 32000 x 1024 by waves of 16 KB each 206 us, by workgroups of
+  // 16 KB whose neighbours run on one XCD 193, and with three of them a CU, which
+  // this much LDS makes it, 170.  (The search for empty rows wants more waves.)
+  const unsigned lds = a.zero_ranks > 0 && a.present ? 52 * 1024 : 0;
+  hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC, ACC>),
+                     dim3((unsigned)(a.run_blocks + a.zero_ranks * a.zero_groups)), dim3(256), lds, ctx->stream, a);
   gift_status st = check_launch("embgrad_sum_kernel");
   if (st != GIFT_OK || a.runs < 2) return st;
   const int64_t ranks = a.run_waves / (a.runs * a.chunks), groups = (a.runs + kJoinWaves - 1) / kJoinWaves;
@@ -902,7 +920,6 @@ gift_status sort_launch(gift_ctx *ctx, const EmbGradJob &j, const GradPlan &p, u
   int bits = 0;
   while ((j.V >> bits) != 0) ++bits;   // the keys are 0 .. V
   gift_status st;
-  uint32_t *present = p.words && !j.accumulate ? reinterpret_cast<uint32_t *>(ws + p.present) : nullptr;
   *cur = 0;
   if (p.tiles == 0) {
     LdsSortArgs a{};
@@ -910,7 +927,7 @@ gift_status sort_launch(gift_ctx *ctx, const EmbGradJob &j, const GradPlan &p, u
     a.wide = j.wide;
     a.key = key[0];
     a.pos = pos[0];
-    a.present = present;
+    a.present = p.words && !j.accumulate ? reinterpret_cast<uint32_t *>(ws + p.present) : nullptr;
     a.T = j.T;
     a.V = j.V;
     a.words = p.words;
@@ -923,10 +940,8 @@ gift_status sort_launch(gift_ctx *ctx, const EmbGradJob &j, const GradPlan &p, u
   }
   SortArgs s{};
   s.hist = reinterpret_cast<uint32_t *>(ws + p.hist);
-  s.present = present;
   s.T = j.T;
   s.V = j.V;
-  s.words = p.words;
   s.tiles = p.tiles;
   s.scanned = p.tiles > kScanTiles;
   const dim3 grid(p.tiles, j.N);
@@ -964,9 +979,10 @@ size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d) {
   return T > 0 ? grad_plan(N, T, V, d).bytes : 0;
 }
 
-int64_t embgrad_waves(const EmbGradJob &j) {
+int64_t embgrad_blocks(const EmbGradJob &j) {
   const int run = run_length(j.N, j.T, j.d);
-  return (int64_t)j.N * ((j.T + run - 1) / run + 3) * column_chunks(j.d, sum_columns(j.d, j.accumulate)) +
+  const int64_t runs = (j.T + run - 1) / run;
+  return (int64_t)j.N * ((runs + 3) / 4 + 1) * column_chunks(j.d, sum_columns(j.d, j.accumulate)) + 8 +
          (j.accumulate ? 0 : (int64_t)j.N * ((j.V + zero_rows_of(j.d) - 1) / zero_rows_of(j.d)));
 }
 
@@ -1002,6 +1018,7 @@ gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &j, char *ws) {
   a.zero_rows = zero_rows_of(j.d);
   a.zero_groups = (j.V + a.zero_rows - 1) / a.zero_rows;
   a.zero_ranks = j.accumulate ? 0 : j.N;
+  a.run_blocks = ((int64_t)blocks_for(a.run_waves) + 7) / 8 * 8;
   a.scale = j.scale;
   if (j.accumulate) return j.bf16 ? sum_launch<uint16_t, true>(ctx, a) : sum_launch<float, true>(ctx, a);
   return j.bf16 ? sum_launch<uint16_t, false>(ctx, a) : sum_launch<float, false>(ctx, a);

@@ -10,6 +10,7 @@
 #include "fp8_e4m3.h"
 #include "gift_internal.h"
 #include "philox.h"
+#include "xcd_map.h"
 
 namespace gift {
 
@@ -482,7 +483,7 @@ gift_status launch_adamw(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *
       const gift_adamw_tensor &x = tensors[i];
       if (x.numel == 0) continue;
       const int64_t more = (x.numel + per_group - 1) / per_group;
-      if (a.count > 0 && chunks + more > 0xffffff) break;   // 2^24 workgroups of 256 threads a launch
+      if (a.count > 0 && chunks + more > kMaxBlocks) break;
       AdamTensor &t = a.t[a.count];
       t.p = x.param;
       t.g = x.grad;
