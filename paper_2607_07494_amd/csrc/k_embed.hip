@@ -39,6 +39,12 @@ __device__ __forceinline__ uint32_t to_bf16(float x) {
   return x != x ? (u >> 16 | 0x40u) : (u + 0x7fffu + (u >> 16 & 1u)) >> 16;
 }
 
+template <bool STREAM, typename W>
+__device__ __forceinline__ W fetch(const W *p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 // VEC neighbouring elements of a row as loaded: converted only where they are
 // used, so that several rows' loads are in flight together.
 template <typename T, int VEC>
@@ -47,11 +53,13 @@ struct RowBits;
 template <int VEC>
 struct RowBits<float, VEC> {
   float x[VEC];
+  // STREAM: past the caches
+  template <bool STREAM = false>
   __device__ __forceinline__ void load(const float *p) {
     if constexpr (VEC >= 4) {
 #pragma unroll
       for (int i = 0; i < VEC; i += 4) {
-        const floatx4_u w = *reinterpret_cast<const floatx4_u *>(p + i);
+        const floatx4_u w = fetch<STREAM>(reinterpret_cast<const floatx4_u *>(p + i));
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[i + k] = w[k];
       }
@@ -66,13 +74,14 @@ struct RowBits<float, VEC> {
 template <int VEC>
 struct RowBits<uint16_t, VEC> {
   uint32_t w[(VEC + 1) / 2];
+  template <bool STREAM = false>
   __device__ __forceinline__ void load(const uint16_t *p) {
     if constexpr (VEC == 8) {
-      const uintx4_u x = *reinterpret_cast<const uintx4_u *>(p);
+      const uintx4_u x = fetch<STREAM>(reinterpret_cast<const uintx4_u *>(p));
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = x[k];
     } else if constexpr (VEC == 4) {
-      const uintx2_u x = *reinterpret_cast<const uintx2_u *>(p);
+      const uintx2_u x = fetch<STREAM>(reinterpret_cast<const uintx2_u *>(p));
 #pragma unroll
       for (int k = 0; k < 2; ++k) w[k] = x[k];
     } else if constexpr (VEC == 2) {
@@ -654,7 +663,7 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
       k[u] = (uint32_t)__builtin_amdgcn_readlane(my_key, i);
       starts[u] = i0 + u < count && (i == 0 || k[u] != (uint32_t)__builtin_amdgcn_readlane(my_key, i > 0 ? i - 1 : 0));
       const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(my_pos, i);
-      x[u].load(dout + (int64_t)p * a.d);
+      x[u].template load<true>(dout + (int64_t)p * a.d);
       if constexpr (ACC)
         if (starts[u]) was[u].load(grads + (int64_t)k[u] * a.d);
     }
@@ -797,11 +806,11 @@ unsigned blocks_for(int64_t waves) { return (unsigned)((waves + 3) / 4); }
 // loads of bfloat16 on wide ones.
 int lane_columns(int64_t d) { return d > 256 ? 8 : d > 128 ? 4 : d > 64 ? 2 : 1; }
 
-// (an accumulating sum holds the old rows too: four columns take half the
-// registers, 65536 x 1536 103 -> 92 us)
-int sum_columns(int64_t d, bool accumulate) {
+// A sum takes at most four: 65536 float32 rows of 1536 in 164 us (eight: 180);
+// an accumulating one holds the old rows too.
+int sum_columns(int64_t d) {
   const int vec = lane_columns(d);
-  return accumulate && vec > 4 ? 4 : vec;
+  return vec > 4 ? 4 : vec;
 }
 
 int64_t column_chunks(int64_t d, int vec) { return (d + 64 * vec - 1) / (64 * vec); }
@@ -812,7 +821,7 @@ size_t a256(size_t b) { return (b + 255) & ~(size_t)255; }
 // to 8 for short ranks, whose time is the longest chain of additions.
 int run_length(int64_t N, int64_t T, int64_t d) {
   int run = 32;
-  while (run > 8 && N * ((T + run - 1) / run) * column_chunks(d, lane_columns(d)) < 2048) run /= 2;
+  while (run > 8 && N * ((T + run - 1) / run) * column_chunks(d, sum_columns(d)) < 2048) run /= 2;
   return run;
 }
 
@@ -906,9 +915,7 @@ gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
 
 template <typename TIn, bool ACC>
 gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
-  const int vec = sum_columns(a.d, ACC);
-  if constexpr (!ACC)
-    if (vec == 8) return sum_launch<TIn, 8, ACC>(ctx, a);
+  const int vec = sum_columns(a.d);
   if (vec == 4) return sum_launch<TIn, 4, ACC>(ctx, a);
   if (vec == 2) return sum_launch<TIn, 2, ACC>(ctx, a);
   return sum_launch<TIn, 1, ACC>(ctx, a);
@@ -982,7 +989,7 @@ size_t embgrad_scratch(int64_t N, int64_t T, int64_t V, int64_t d) {
 int64_t embgrad_blocks(const EmbGradJob &j) {
   const int run = run_length(j.N, j.T, j.d);
   const int64_t runs = (j.T + run - 1) / run;
-  return (int64_t)j.N * ((runs + 3) / 4 + 1) * column_chunks(j.d, sum_columns(j.d, j.accumulate)) + 8 +
+  return (int64_t)j.N * ((runs + 3) / 4 + 1) * column_chunks(j.d, sum_columns(j.d)) + 8 +
          (j.accumulate ? 0 : (int64_t)j.N * ((j.V + zero_rows_of(j.d) - 1) / zero_rows_of(j.d)));
 }
 
@@ -1013,7 +1020,7 @@ gift_status launch_embgrad(gift_ctx *ctx, const EmbGradJob &j, char *ws) {
   a.words = p.words;
   a.run = p.run;
   a.runs = p.runs;
-  a.chunks = column_chunks(j.d, sum_columns(j.d, j.accumulate));
+  a.chunks = column_chunks(j.d, sum_columns(j.d));
   a.run_waves = (int64_t)j.N * p.runs * a.chunks;
   a.zero_rows = zero_rows_of(j.d);
   a.zero_groups = (j.V + a.zero_rows - 1) / a.zero_rows;
