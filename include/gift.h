@@ -404,7 +404,8 @@ gift_status gift_decode_batch(gift_ctx *ctx, int32_t count, const gift_factor *c
  * be reallocated by a later call, and is refused while the stream is being
  * captured (GIFT_EUNSUPPORTED); a captured call passes scratch of the caller's
  * that lives as long as the graph and that no other work uses while the graph
- * runs.  The device that the context is bound to must be current (GIFT_EINVAL).
+ * runs.  Captured launches are left out of the per-kernel timing.  The device
+ * that the context is bound to must be current (GIFT_EINVAL).
  * ------------------------------------------------------------------------- */
 
 /* Integer type of token ids. */
@@ -468,7 +469,7 @@ uint64_t gift_embedding_grad_scratch(int32_t N, int64_t T, int64_t V, int64_t d)
  * Squares and sums are float64.  out + 1 is the grad_scale of gift_adamw_step.
  * Errors: GIFT_EINVAL (NULL, bad type, max_norm not > 0, scratch too small or
  * misaligned, a gradient not aligned to its element), GIFT_ESHAPE (count < 0, an
- * element count outside [0, 2^34]), GIFT_EUNSUPPORTED (scratch NULL under
+ * element count outside [0, 2^33]), GIFT_EUNSUPPORTED (scratch NULL under
  * capture). */
 gift_status gift_grad_norm(gift_ctx *ctx, int32_t count, const void *const *grads,
                            const int64_t *numel, gift_dtype dtype, double max_norm, float *out,
@@ -534,7 +535,7 @@ typedef struct {
  * Errors: GIFT_EINVAL (NULL, bad type, misaligned; lr or a weight decay not
  * finite or negative, a beta outside [0, 1), eps not a normal positive
  * float32, step < 1 without step_dev), GIFT_ESHAPE (count < 0, numel outside
- * [0, 2^34]). */
+ * [0, 2^33]). */
 gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *tensors,
                             const gift_adamw_options *options);
 

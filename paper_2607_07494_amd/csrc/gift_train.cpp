@@ -14,7 +14,7 @@ namespace {
 constexpr int64_t kMaxIds = (1LL << 31) - 1;       // positions of all ranks; sort places are 32-bit
 constexpr int64_t kMaxVocab = (1LL << 31) - 2;
 constexpr int64_t kMaxWidth = 1LL << 20;
-constexpr int64_t kMaxElements = 1LL << 34;
+constexpr int64_t kMaxElements = 1LL << 33;      // of a tensor: one launch takes its chunks
 
 bool aligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
@@ -33,6 +33,23 @@ gift_status enter(gift_ctx *ctx, const char *call) {
   if (dev != ctx->device) return fail(GIFT_EINVAL, call, "the context's device is not the current one");
   return GIFT_OK;
 }
+
+// No events are recorded into a graph: while the stream is being captured the
+// call's launches are not timed.
+struct QuietCapture {
+  gift_ctx *ctx;
+  bool was;
+  explicit QuietCapture(gift_ctx *c) : ctx(c), was(c->no_alloc_call) {
+    if (!ctx->profile) return;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(ctx->stream, &capture) != hipSuccess) {
+      (void)hipGetLastError();
+      return;
+    }
+    if (capture != hipStreamCaptureStatusNone) ctx->no_alloc_call = true;
+  }
+  ~QuietCapture() { ctx->no_alloc_call = was; }
+};
 
 // the caller's scratch, or the context's workspace outside of a capture
 gift_status take_scratch(gift_ctx *ctx, const char *call, void *scratch, uint64_t have, size_t need, uintptr_t align,
@@ -93,6 +110,7 @@ gift_status gift_embedding(gift_ctx *ctx, const void *table, gift_dtype table_dt
   j.table_bf16 = table_dtype == GIFT_BF16;
   j.out_bf16 = out_dtype == GIFT_BF16;
   j.wide = token_type == GIFT_I64;
+  QuietCapture quiet(ctx);
   return launch_lookup(ctx, j);
 }
 
@@ -135,6 +153,7 @@ gift_status gift_embedding_grad(gift_ctx *ctx, const void *tokens, gift_index_ty
   void *ws = nullptr;
   if (T > 0 && (st = take_scratch(ctx, call, scratch, scratch_bytes, embgrad_scratch(N, T, V, d), 256, &ws)) != GIFT_OK)
     return st;
+  QuietCapture quiet(ctx);
   return launch_embgrad(ctx, j, static_cast<char *>(ws));
 }
 
@@ -148,7 +167,7 @@ gift_status gift_grad_norm(gift_ctx *ctx, int32_t count, const void *const *grad
   if (count > 0 && (!grads || !numel)) return fail(GIFT_EINVAL, call, "NULL argument");
   for (int32_t i = 0; i < count; ++i) {
     if (numel[i] < 0 || numel[i] > kMaxElements)
-      return fail(GIFT_ESHAPE, call, "element counts must be in [0, 2^34]");
+      return fail(GIFT_ESHAPE, call, "element counts must be in [0, 2^33]");
     if (numel[i] > 0 && !grads[i]) return fail(GIFT_EINVAL, call, "NULL gradient");
     if (!aligned(grads[i], dtype == GIFT_F32 ? 4 : 2))
       return fail(GIFT_EINVAL, call, "a gradient is not aligned to its element");
@@ -158,6 +177,7 @@ gift_status gift_grad_norm(gift_ctx *ctx, int32_t count, const void *const *grad
   if (st != GIFT_OK) return st;
   void *part = nullptr;
   if ((st = take_scratch(ctx, call, scratch, scratch_bytes, grad_norm_scratch(), 8, &part)) != GIFT_OK) return st;
+  QuietCapture quiet(ctx);
   return launch_grad_norm(ctx, count, grads, numel, dtype == GIFT_BF16, max_norm, out, static_cast<double *>(part));
 }
 
@@ -183,7 +203,7 @@ gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tenso
   for (int32_t i = 0; i < count; ++i) {
     const gift_adamw_tensor &t = tensors[i];
     if (t.numel < 0 || t.numel > kMaxElements)
-      return fail(GIFT_ESHAPE, call, "element counts must be in [0, 2^34]");
+      return fail(GIFT_ESHAPE, call, "element counts must be in [0, 2^33]");
     if (t.numel == 0) continue;
     if (!t.param || !t.grad || !t.m || !t.v || (eight && (!t.m_scales || !t.v_scales)))
       return fail(GIFT_EINVAL, call, "NULL tensor");
@@ -195,6 +215,7 @@ gift_status gift_adamw_step(gift_ctx *ctx, int32_t count, const gift_adamw_tenso
   }
   gift_status st = enter(ctx, call);
   if (st != GIFT_OK) return st;
+  QuietCapture quiet(ctx);
   return launch_adamw(ctx, count, tensors, o);
 }
 

@@ -11,7 +11,7 @@
 // in float32 and stores every row that begins and ends in its run; the parts of
 // rows that cross a border go to scratch and a second kernel adds them in a
 // fixed order.  No atomics on values: the same inputs give the same bits.  Rows
-// without a token are zeroed by further waves of the same launch.
+// without a token are zeroed by further workgroups of the same launch.
 //
 // Ids outside [0, V) (padding) get the sort key V, the largest: they end up
 // behind all others and nothing reads them.

@@ -764,7 +764,8 @@ class AdamW:
         number from 1 (default: one more than the last one's), or an int64
         tensor of one element, which the caller advances.  A captured step needs
         both as tensors where they change from replay to replay.
-        ``grad_scale``: a float32 tensor of one element; NaN skips the step.
+        ``grad_scale``: a float32 tensor of one element; NaN skips the step (which
+        counts all the same: the host does not know).
         """
         grads = list(grads)
         if len(grads) != len(self.params):

@@ -93,6 +93,16 @@ def test_norm_corners(ctx):
     assert math.isnan(a) and math.isnan(b)
 
 
+def test_norm_of_more_than_32_bits_of_elements(ctx):
+    n = 2 ** 31 + 4099
+    x = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    x[[0, 2 ** 31 - 1, 2 ** 31, n - 1]] = torch.tensor([1.0, 2.0, 4.0, 8.0], dtype=torch.bfloat16, device=DEV)
+    out = torch.empty(2, device=DEV)
+    gift.grad_norm(ctx, [x[1:], x[:1]], out)
+    torch.cuda.synchronize()
+    assert abs(out[0].item() - math.sqrt(85)) <= 2.0 ** -23 * math.sqrt(85)
+
+
 # ---------------------------------------------------------------------------
 # AdamW
 # ---------------------------------------------------------------------------
@@ -349,6 +359,27 @@ def test_captured_steps_advance_by_device_scalars(ctx):
             assert abs(got[0] - norm) <= 2.0 ** -23 * norm and abs(got[1] - coef) <= 2.0 ** -23 * coef
             c.oracle_step(grads, float(F(LR * k)), k, float(got[1]))
             c.check()
+    other.close()
+
+
+def test_captured_launches_are_not_timed(ctx):
+    """With per-kernel timing on, a captured step replays as it is and later eager steps are timed."""
+    s = torch.cuda.Stream()
+    other = gift.Context(stream=s.cuda_stream)
+    p, g = torch.ones(5000, device=DEV), torch.ones(5000, device=DEV)
+    opt = gift.AdamW(other, [p])
+    other.profile(True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        opt.step([g], lr=0.5, step=1)
+    assert other.profile_read("optimizer")[0] == 0
+    graph.replay()
+    torch.cuda.synchronize()
+    np.testing.assert_allclose(p.cpu().numpy(), 0.5, rtol=1e-6)      # the first step moves by lr
+    opt.step([g], lr=0.0, step=2)
+    launches, ms = other.profile_read("optimizer")
+    assert launches == 1 and ms > 0
     other.close()
 
 

@@ -160,6 +160,8 @@ CASES = [
     (1, 300, 1_048_576, 3, "f32", 64, "outside"),
     (2, 5000, 140_000, 9, "bf16", 64, "outside"),
     (1, 9000, 3, 1030, "bf16", 64, "one"),
+    (2, 40, 30, 5000, "bf16", 64, "few"),
+    (300, 5, 7, 3, "f32", 32, "outside"),
 ]
 
 

@@ -77,7 +77,7 @@ NORM = dict(count=2, grads=(ctypes.c_void_p * 2)(0x1000, 0x2000), numel=(ctypes.
     (dict(grads=None), E, "NULL"), (dict(numel=None), E, "NULL"), (dict(out=None), E, "NULL"), (dict(out=ODD), E, "aligned"),
     (dict(dt=3), E, "dtype"), (dict(max_norm=0.0), E, "max_norm"), (dict(max_norm=NAN), E, "max_norm"),
     (dict(count=-1), S, "count"), (dict(numel=(ctypes.c_int64 * 2)(4, -1)), S, "element counts"),
-    (dict(numel=(ctypes.c_int64 * 2)(4, (1 << 34) + 1)), S, "element counts"),
+    (dict(numel=(ctypes.c_int64 * 2)(4, (1 << 33) + 1)), S, "element counts"),
     (dict(grads=(ctypes.c_void_p * 2)(0x1000, None)), E, "NULL"), (dict(grads=(ctypes.c_void_p * 2)(0x1000, 0x2002)), E, "aligned"),
 ])
 def test_grad_norm(ctx, change, status, word):
@@ -104,7 +104,7 @@ def _step(ctx, tensor=None, count=1, null=False, **options):
     (dict(lr_dev=0x1002), E, "scalar"), (dict(step_dev=0x1004), E, "scalar"), (dict(grad_scale=0x1001), E, "scalar"),
     (dict(tensor=dict(param=None)), E, "NULL"), (dict(tensor=dict(grad=None)), E, "NULL"), (dict(tensor=dict(m=None)), E, "NULL"),
     (dict(tensor=dict(v_scales=None), moments=1), E, "NULL"),
-    (dict(tensor=dict(numel=-1)), S, "element counts"), (dict(tensor=dict(weight_decay=-0.1)), E, "weight decays"),
+    (dict(tensor=dict(numel=-1)), S, "element counts"), (dict(tensor=dict(numel=(1 << 33) + 1)), S, "element counts"), (dict(tensor=dict(weight_decay=-0.1)), E, "weight decays"),
     (dict(tensor=dict(weight_decay=INF)), E, "weight decays"), (dict(tensor=dict(param=0x1002)), E, "aligned"),
     (dict(tensor=dict(v=0x1002)), E, "aligned"), (dict(tensor=dict(copy=0x1001)), E, "aligned"),
     (dict(tensor=dict(m_scales=0x1002), moments=1), E, "aligned"), (dict(tensor=dict(grad=0x1001), grad_dtype=1), E, "aligned"),
