@@ -501,7 +501,8 @@ typedef struct {
   gift_moments moments;
   const float *lr_dev;        /* NULL, or the learning rate on the device (before lr)   */
   const int64_t *step_dev;    /* NULL, or the step on the device (before step): not     */
-                              /* written; a captured step advances it by itself         */
+                              /* written, the caller advances it; below 1 it skips the  */
+                              /* step                                                   */
   const float *grad_scale;    /* NULL, or a factor of every gradient on the device; NaN */
                               /* skips the step: nothing is written                     */
 } gift_adamw_options;

@@ -177,12 +177,14 @@ __host__ __device__ __forceinline__ void bias_corrections(double lr, int64_t ste
 __device__ __forceinline__ AdamStep adam_step(const AdamArgs &a, const AdamTensor &t, float &keep) {
   AdamStep s = a.host;
   keep = t.keep;
+  s.gscale = a.grad_scale ? *a.grad_scale : 1.0f;
   if (a.lr_dev || a.step_dev) {
     const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
-    bias_corrections(lr, a.step_dev ? *a.step_dev : a.step, a.log_beta1, a.log_beta2, s);
+    const int64_t step = a.step_dev ? *a.step_dev : a.step;
+    bias_corrections(lr, step, a.log_beta1, a.log_beta2, s);
     keep = (float)(1.0 - lr * t.decay);
+    if (step < 1) s.gscale = __uint_as_float(0x7fc00000u);   // no such step: skipped
   }
-  s.gscale = a.grad_scale ? *a.grad_scale : 1.0f;
   return s;
 }
 

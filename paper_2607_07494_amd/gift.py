@@ -175,6 +175,7 @@ class Context:
             stream = torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
         self._h = ctypes.c_void_p()
         self._factors = weakref.WeakSet()
+        self._stream = int(stream)
         _check(LIB.gift_ctx_create(ctypes.c_void_p(int(stream)), ctypes.byref(self._h)))
 
     @property
@@ -183,6 +184,7 @@ class Context:
 
     def set_stream(self, stream):
         _check(LIB.gift_ctx_set_stream(self._h, ctypes.c_void_p(int(stream))))
+        self._stream = int(stream)
 
     def set_statistics_event(self, event):
         """Record ``event`` (a torch.cuda.Event, or None) after the statistics
@@ -685,6 +687,7 @@ class AdamW:
             raise ValueError(f"moments must be one of {sorted(MOMENTS)}, not {moments!r}")
         self.ctx, self.params, self.betas, self.eps, self.moments = ctx, list(params), betas, eps, moments
         self.seed, self.steps = seed, 0
+        self._owns_state = False
         count = len(self.params)
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
         self.copies = list(copies) if copies is not None else [None] * count
@@ -709,7 +712,8 @@ class AdamW:
             _on_current_device(parameter=p)
             if c is not None:
                 _on_current_device(copy=c)
-        if state is None:
+        own_state = state is None
+        if own_state:
             dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
             state = {name: torch.zeros(n, dtype=dtype, device=dev) for name, (n, dtype) in sizes.items()}
             if count:
@@ -717,6 +721,7 @@ class AdamW:
                 torch.cuda.current_stream().synchronize()
         elif count:
             _on_current_device(**state)
+        self._owns_state = own_state and count > 0
         self.state = dict(state)
         spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
                  for t in self.params + [c for c in self.copies if c is not None] + list(self.state.values())]
@@ -762,12 +767,15 @@ class AdamW:
 
         ``lr``: a number, or a float32 tensor of one element.  ``step``: the step's
         number from 1 (default: one more than the last one's), or an int64
-        tensor of one element, which the caller advances.  A captured step needs
+        tensor of one element, which the caller advances (below 1 it skips the
+        step).  A captured step needs
         both as tensors where they change from replay to replay.
         ``grad_scale``: a float32 tensor of one element; NaN skips the step (which
         counts all the same: the host does not know).
         """
         grads = list(grads)
+        if self._tensors is None:
+            raise GiftError(EINVAL, "the optimizer is closed")
         if len(grads) != len(self.params):
             raise ValueError("grads must have one entry per parameter")
         shapes = list(map(_SHAPE, grads))
@@ -796,3 +804,16 @@ class AdamW:
         _check(LIB.gift_adamw_step(self.ctx._h, len(grads), self._tensors, ctypes.byref(o)))
         if not on_device:
             self.steps = number
+
+    def close(self):
+        """Wait for the context's stream, if the moments are this object's own, and let go of them."""
+        if self._owns_state and self.ctx._h:
+            torch.cuda.ExternalStream(self.ctx._stream).synchronize()
+        self._owns_state, self.state, self._tensors, self.params = False, {}, None, []
+        self._shapes, self._grad_words = None, None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -280,6 +280,8 @@ def test_a_nan_factor_skips_the_step(ctx):
         c.check()
         c.opt.step(grads, lr=LR, step=2, grad_scale=torch.full((1,), float("nan"), device=DEV))
         c.check()
+        c.opt.step(grads, lr=LR, step=torch.zeros(1, dtype=torch.int64, device=DEV))      # no step 0
+        c.check()
 
 
 def test_a_nan_gradient_stays_in_its_place(ctx):
@@ -401,6 +403,24 @@ def test_state_tensors_are_used_in_place_and_overlap_is_refused(ctx):
         gift.AdamW(ctx, [torch.zeros((6, 4), device=DEV)]).step([torch.zeros((4, 6), device=DEV).t()], lr=LR)
     with pytest.raises(TypeError, match="one dtype"):
         gift.grad_norm(ctx, [p, p.bfloat16()], torch.empty(2, device=DEV))
+
+
+def test_closing(ctx):
+    p, g = torch.ones(300, device=DEV), torch.ones(300, device=DEV)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    other = gift.Context(stream=s.cuda_stream)
+    opt = gift.AdamW(other, [p])
+    opt.step([g], lr=0.5)
+    opt.close()                      # waits for the step
+    np.testing.assert_allclose(p.cpu().numpy(), 0.5, rtol=1e-6)
+    with pytest.raises(gift.GiftError, match="closed"):
+        opt.step([g], lr=0.5)
+    opt = gift.AdamW(other, [p])
+    other.close()
+    with pytest.raises(gift.GiftError, match="NULL"):
+        opt.step([g], lr=0.5)
+    opt.close()
 
 
 def test_elements_past_32_bits(ctx):
