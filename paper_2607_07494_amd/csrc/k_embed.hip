@@ -358,10 +358,9 @@ __global__ __launch_bounds__(WAVES * 64) void sort_lds_kernel(LdsSortArgs a) {
   }
 }
 
-constexpr int kSortThreads = 256;
-constexpr int kSortPerWave = 512;                      // keys of a wave, in order
-constexpr int kSortTile = 4 * kSortPerWave;            // keys of a workgroup
-
+constexpr int kSortWaves = 8, kSortThreads = kSortWaves * 64;
+constexpr int kSortPerWave = 256;                      // keys of a wave, in order
+constexpr int kSortTile = kSortWaves * kSortPerWave;   // keys of a workgroup
 constexpr int kSortItems = kSortTile / kSortThreads;
 // Up to this many tiles a scattering workgroup sums their counts itself (65536
 // positions: a launch between the two took 8.6 us a pass, this adds 1).
@@ -386,7 +385,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t rank, in
 __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(SortArgs a) {
   __shared__ uint32_t count[kDigits];
   const int64_t rank = blockIdx.y;
-  count[threadIdx.x] = 0;
+  if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * kSortTile + threadIdx.x;
   uint32_t key[kSortItems];
@@ -398,10 +397,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_hist_kernel(SortArgs a) {
     if (lo + it * kSortThreads < a.T) atomicAdd(&count[(key[it] >> a.shift) & 255u], 1u);
   }
   __syncthreads();
-  a.hist[(rank * a.tiles + blockIdx.x) * kDigits + threadIdx.x] = count[threadIdx.x];
+  if (threadIdx.x < kDigits) a.hist[(rank * a.tiles + blockIdx.x) * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
-// exclusive prefix sums over 256 digits, one a thread
+// exclusive prefix sums over 256 digits, one a thread of the first four waves
 __device__ __forceinline__ uint32_t digits_before(uint32_t count, uint32_t wave_sum[4]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   uint32_t s = count;
@@ -410,9 +409,9 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t count, uint32_t wave_
     const uint32_t t = (uint32_t)__shfl_up((int)s, o);
     if (lane >= o) s += t;
   }
-  if (lane == 63) wave_sum[wave] = s;
+  if (lane == 63 && wave < 4) wave_sum[wave] = s;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) s += wave_sum[w];
+  for (int w = 0; w < wave && w < 4; ++w) s += wave_sum[w];
   return s - count;
 }
 
@@ -420,6 +419,7 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t count, uint32_t wave_
 // digit's tiles in four quarters, eight loads in flight
 __global__ __launch_bounds__(4 * kDigits) void sort_scan_kernel(uint32_t *hist, int tiles) {
   __shared__ uint32_t quarter_sum[4][kDigits];
+  __shared__ uint32_t first[kDigits];
   __shared__ uint32_t wave_sum[4];
   const int digit = threadIdx.x % kDigits, quarter = threadIdx.x / kDigits, share = (tiles + 3) / 4;
   const int from = quarter * share, to = from + share < tiles ? from + share : tiles;
@@ -434,24 +434,11 @@ __global__ __launch_bounds__(4 * kDigits) void sort_scan_kernel(uint32_t *hist, 
     if (q < quarter) before += quarter_sum[q][digit];
     total += quarter_sum[q][digit];
   }
+  // (the first quarter's threads are the first four waves)
+  const uint32_t digit_first = digits_before(total, wave_sum);
+  if (quarter == 0) first[digit] = digit_first;
   __syncthreads();
-  if (quarter == 0) quarter_sum[0][digit] = total;
-  __syncthreads();
-  // every digit's first place, by the first four waves
-  uint32_t at = 0;
-  {
-    const int lane = threadIdx.x & 63, wave = digit / 64;
-    uint32_t s = quarter_sum[0][digit];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t t = (uint32_t)__shfl_up((int)s, o);
-      if (lane >= o) s += t;
-    }
-    if (lane == 63 && quarter == 0) wave_sum[wave] = s;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) s += wave_sum[w];
-    at = s - quarter_sum[0][digit] + before;
-  }
+  uint32_t at = first[digit] + before;
   for (int t0 = from; t0 < to; t0 += 8) {
     uint32_t c[8];
 #pragma unroll
@@ -464,15 +451,14 @@ __global__ __launch_bounds__(4 * kDigits) void sort_scan_kernel(uint32_t *hist, 
   }
 }
 
-// Stable scatter: a wave walks its 512 keys in order, 64 at a time; a key's
+// Stable scatter: a wave walks its keys in order, 64 at a time; a key's
 // place is its digit's next free place plus the equal digits in lower lanes.
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) {
-  __shared__ uint32_t next[4][kDigits];
+  __shared__ uint32_t next[kSortWaves][kDigits];
   __shared__ uint32_t wave_sum[4];
   const int64_t rank = blockIdx.y;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) next[w][threadIdx.x] = 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, digit_of = threadIdx.x % kDigits;
+  for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) next[0][i] = 0;
   const int64_t lo = (int64_t)blockIdx.x * kSortTile + wave * kSortPerWave;
   uint32_t key[kSortItems], pos[kSortItems];
 #pragma unroll
@@ -481,8 +467,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
     key[it] = i < a.T ? sort_key(a, rank, i) : 0u;
     pos[it] = a.tokens || i >= a.T ? (uint32_t)i : a.pos_in[rank * a.T + i];
   }
-  // the tile's first place of digit threadIdx.x
-  const uint32_t *h = a.hist + rank * a.tiles * kDigits + threadIdx.x;
+  // the tile's first place of digit digit_of (its second half of the threads does the same and keeps nothing)
+  const uint32_t *h = a.hist + rank * a.tiles * kDigits + digit_of;
   uint32_t first;
   if (a.scanned) {
     first = h[(int64_t)blockIdx.x * kDigits];
@@ -519,11 +505,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
     order[it] = seen + before;
   }
   __syncthreads();
+  if (threadIdx.x < kDigits) {
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t c = next[w][threadIdx.x];
-    next[w][threadIdx.x] = first;
-    first += c;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = next[w][digit_of];
+      next[w][digit_of] = first;
+      first += c;
+    }
   }
   __syncthreads();
   uint32_t *key_out = a.key_out + rank * a.T, *pos_out = a.pos_out + rank * a.T;
