@@ -629,23 +629,27 @@ def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumu
 GRAD_NORM_SCRATCH_BYTES = 16384
 
 
-def _gradient_list(grads):
-    """``(dtype, data pointers)`` of a list of gradients on the current device, of one dtype.
+def _all_on_current_device(tensors, name):
+    """Raise ValueError unless every tensor of a list is contiguous and on the current device.
 
     Loops of C functions: a model has hundreds of tensors, and a step's kernels
     take less time than hundreds of passes through Python."""
-    T = torch.Tensor
+    devices = set(map(torch.Tensor.get_device, tensors))
+    if devices and min(devices) < 0:
+        raise ValueError(f"{name} must be GPU tensors")
+    if devices and devices != {torch.cuda.current_device()}:
+        raise ValueError(f"{name} must be on the current device, not on {devices}")
+    if not all(map(torch.Tensor.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _gradient_list(grads):
+    """``(dtype, data pointers)`` of a list of gradients on the current device, of one dtype."""
     dt = _value_dtype(grads[0], "gradients")
     if len(set(map(_DTYPE, grads))) > 1:
         raise TypeError(f"gradients must have one dtype: {set(map(_DTYPE, grads))}")
-    devices = set(map(T.get_device, grads))
-    if min(devices) < 0:
-        raise ValueError("gradients must be GPU tensors")
-    if devices != {torch.cuda.current_device()}:
-        raise ValueError(f"gradients must be on the current device, not on {devices}")
-    if not all(map(T.is_contiguous, grads)):
-        raise ValueError("gradients must be contiguous")
-    return dt, array.array("Q", map(T.data_ptr, grads))
+    _all_on_current_device(grads, "gradients")
+    return dt, array.array("Q", map(torch.Tensor.data_ptr, grads))
 
 
 def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=None):
@@ -693,13 +697,14 @@ class AdamW:
         self.copies = list(copies) if copies is not None else [None] * count
         if len(decay) != count or len(self.copies) != count:
             raise ValueError("weight_decay and copies must have one entry per parameter")
-        for p, c in zip(self.params, self.copies):
-            if p.dtype != torch.float32:
-                raise TypeError(f"parameters must be float32, not {p.dtype}")
-            if c is not None:
-                _expect(c, p.shape, "a copy")
-                if c.dtype != torch.bfloat16:
-                    raise TypeError(f"copies must be bfloat16, not {c.dtype}")
+        given = [c for c in self.copies if c is not None]
+        for name, tensors, dtype in (("parameters", self.params, torch.float32), ("copies", given, torch.bfloat16)):
+            if any(d != dtype for d in map(_DTYPE, tensors)):
+                raise TypeError(f"{name} must be {str(dtype)[6:]}, not {set(map(_DTYPE, tensors)) - {dtype}}")
+        self._shapes = list(map(_SHAPE, self.params))
+        for shape, c in zip(self._shapes, self.copies):
+            if c is not None and c.shape != shape:
+                _expect(c, shape, "a copy")
         sizes = self.state_sizes(self.params, moments)
         if state is not None:
             if set(state) != set(sizes):
@@ -708,10 +713,8 @@ class AdamW:
                 _expect(state[name], (n,), f"state[{name!r}]")
                 if state[name].dtype != dtype:
                     raise TypeError(f"state[{name!r}] must have dtype {dtype}, not {state[name].dtype}")
-        for p, c in zip(self.params, self.copies):
-            _on_current_device(parameter=p)
-            if c is not None:
-                _on_current_device(copy=c)
+        _all_on_current_device(self.params, "parameters")
+        _all_on_current_device(given, "copies")
         own_state = state is None
         if own_state:
             dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
@@ -723,25 +726,35 @@ class AdamW:
             _on_current_device(**state)
         self._owns_state = own_state and count > 0
         self.state = dict(state)
-        spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                 for t in self.params + [c for c in self.copies if c is not None] + list(self.state.values())]
-        spans = sorted(s for s in spans if s[1] > s[0])
-        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+        everything = self.params + given + list(self.state.values())
+        begins, ends = list(map(torch.Tensor.data_ptr, everything)), []
+        for begin, t in zip(begins, everything):
+            ends.append(begin + t.nbytes)
+        spans = sorted(x for x in zip(begins, ends) if x[1] > x[0])
+        if any(x[1] > y[0] for x, y in zip(spans, spans[1:])):
             raise ValueError("parameters, copies and moments must not overlap")
         self.starts = self._starts(self.params)[0]
         self._tensors = (_AdamWTensor * count)()
-        for x, p, c, at, wd in zip(self._tensors, self.params, self.copies, self.starts, decay):
-            x.param, x.numel, x.weight_decay = p.data_ptr(), p.numel(), wd
-            x.copy = c.data_ptr() if c is not None else None
-            for name in ("m", "v"):
-                s = self.state[name]
-                setattr(x, name, s.data_ptr() + at * s.element_size())
-                if moments == "e4m3":
-                    setattr(x, name + "_scales", self.state[name + "_scales"].data_ptr() + at // self.BLOCK * 4)
-        # the tensors' gradient fields, as 64-bit words
+        # the tensors' fields, as 64-bit words
         words = memoryview(self._tensors).cast("B").cast("Q") if count else memoryview(array.array("Q"))
-        self._grad_words = words[_AdamWTensor.grad.offset // 8::ctypes.sizeof(_AdamWTensor) // 8]
-        self._shapes = list(map(_SHAPE, self.params))
+        stride = ctypes.sizeof(_AdamWTensor) // 8
+
+        def field(name):
+            return words[getattr(_AdamWTensor, name).offset // 8::stride]
+
+        def fill(name, values, typecode="Q"):
+            field(name)[:] = memoryview(array.array(typecode, values)).cast("B").cast("Q")
+
+        fill("param", begins[:count])
+        fill("numel", map(torch.Tensor.numel, self.params))
+        fill("weight_decay", decay, "d")
+        if given:
+            fill("copy", [0 if c is None else c.data_ptr() for c in self.copies])
+        for name, t in self.state.items():
+            per = self.BLOCK if name.endswith("_scales") else 1
+            base, size = t.data_ptr(), t.element_size()
+            fill(name, [base + at // per * size for at in self.starts])
+        self._grad_words = field("grad")
         self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
                                       moments=MOMENTS[moments])
 
