@@ -437,7 +437,7 @@ gift_status gift_embedding(gift_ctx *ctx, const void *table, gift_dtype table_dt
  *   scratch NULL or 256-byte aligned device memory of at least
  *           gift_embedding_grad_scratch(N, T, V, d) bytes, scratch_bytes of it.
  * Positions are ordered by token (a stable sort), a row's terms are added in
- * float32 in runs of neighbouring positions, the runs' sums in order: the same
+ * float32 in runs of neighbouring positions, the runs' sums in a fixed order: the same
  * inputs give the same bits.  T may be 0.  Any element alignment of dout and
  * grads.
  * Errors: GIFT_EINVAL (NULL, bad type, scale not finite, scratch too small or
