@@ -33,7 +33,7 @@ KERNELS = {
     "embed": 15, "embed_grad": 16, "norm": 17, "optimizer": 18,
 }
 I32, I64 = 0, 1
-_DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
+_DTYPE, _SHAPE, _NBYTES = (operator.attrgetter(name) for name in ("dtype", "shape", "nbytes"))
 MOMENTS = {"f32": 0, "e4m3": 1}
 
 _STATUS = {OK: "GIFT_OK", EINVAL: "GIFT_EINVAL", ESHAPE: "GIFT_ESHAPE", ENOMEM: "GIFT_ENOMEM",
@@ -671,6 +671,16 @@ def grad_norm(ctx: Context, grads, out, max_norm: float = float("inf"), scratch=
                               out.data_ptr(), ws, ws_bytes))
 
 
+def _scalar(x, dtype, name):
+    """Address of a tensor of one element on the current device, else None."""
+    if not isinstance(x, torch.Tensor):
+        return None
+    if x.dtype != dtype or x.numel() != 1:
+        raise TypeError(f"{name} must be one {dtype} element")
+    _on_current_device(**{name: x})
+    return x.data_ptr()
+
+
 class AdamW:
     """AdamW over a list of float32 tensors (``gift_adamw_step``).
 
@@ -681,6 +691,12 @@ class AdamW:
     tensors used in place (:meth:`state_sizes`); made as zeros when not given.
     Tensor i's elements lie in ``m`` and ``v`` from ``starts[i]`` on (a multiple of
     512), its scales in ``m_scales`` and ``v_scales`` from ``starts[i] // 256``.
+
+    ``params``, ``copies`` and ``state`` may change between steps: a step works on the
+    tensors that they hold, where those lie, at the time of the call (after
+    ``param.data = other`` or ``state["m"] = loaded`` on the other memory).  Shapes
+    and dtypes must stay.  A captured step keeps the addresses
+    that it was captured with.
     """
 
     ALIGN, BLOCK = 512, 256
@@ -691,22 +707,55 @@ class AdamW:
             raise ValueError(f"moments must be one of {sorted(MOMENTS)}, not {moments!r}")
         self.ctx, self.params, self.betas, self.eps, self.moments = ctx, list(params), betas, eps, moments
         self.seed, self.steps = seed, 0
-        self._owns_state = False
+        self._own = []          # moments made here
         count = len(self.params)
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
         self.copies = list(copies) if copies is not None else [None] * count
         if len(decay) != count or len(self.copies) != count:
             raise ValueError("weight_decay and copies must have one entry per parameter")
+        self._shapes = list(map(_SHAPE, self.params))
+        self.starts = self._starts(self.params)[0]
+        self._tensors = (_AdamWTensor * count)()
+        # the tensors' fields, as 64-bit words
+        self._words = memoryview(self._tensors).cast("B").cast("Q") if count else memoryview(array.array("Q"))
+        self._check_tensors(state)
+        if state is None:
+            dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
+            state = {name: torch.zeros(n, dtype=dtype, device=dev)
+                     for name, (n, dtype) in self.state_sizes(self.params, moments).items()}
+            if count:
+                # the zeros are written on torch's stream, the steps run on the context's
+                torch.cuda.current_stream().synchronize()
+                self._own = list(state.values())
+        self.state = dict(state)
+        self._fill("numel", map(torch.Tensor.numel, self.params))
+        self._fill("weight_decay", decay, "d")
+        self._bind()
+        self._grad_words = self._field("grad")
+        self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
+                                      moments=MOMENTS[moments])
+
+    def _field(self, name):
+        return self._words[getattr(_AdamWTensor, name).offset // 8::ctypes.sizeof(_AdamWTensor) // 8]
+
+    def _fill(self, name, values, typecode="Q"):
+        self._field(name)[:] = memoryview(array.array(typecode, values)).cast("B").cast("Q")
+
+    def _check_tensors(self, state):
+        """Raise unless params, copies and state (None: still to be made) can be used."""
         given = [c for c in self.copies if c is not None]
         for name, tensors, dtype in (("parameters", self.params, torch.float32), ("copies", given, torch.bfloat16)):
             if any(d != dtype for d in map(_DTYPE, tensors)):
                 raise TypeError(f"{name} must be {str(dtype)[6:]}, not {set(map(_DTYPE, tensors)) - {dtype}}")
-        self._shapes = list(map(_SHAPE, self.params))
-        for shape, c in zip(self._shapes, self.copies):
+        if len(self.params) != len(self._shapes) or len(self.copies) != len(self._shapes):
+            raise ValueError("params and copies must keep their lengths")
+        for shape, p, c in zip(self._shapes, self.params, self.copies):
+            if p.shape != shape:
+                _expect(p, shape, "a parameter")
             if c is not None and c.shape != shape:
                 _expect(c, shape, "a copy")
-        sizes = self.state_sizes(self.params, moments)
         if state is not None:
+            sizes = self.state_sizes(self.params, self.moments)
             if set(state) != set(sizes):
                 raise ValueError(f"state must hold {sorted(sizes)}, not {sorted(state)}")
             for name, (n, dtype) in sizes.items():
@@ -715,48 +764,43 @@ class AdamW:
                     raise TypeError(f"state[{name!r}] must have dtype {dtype}, not {state[name].dtype}")
         _all_on_current_device(self.params, "parameters")
         _all_on_current_device(given, "copies")
-        own_state = state is None
-        if own_state:
-            dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
-            state = {name: torch.zeros(n, dtype=dtype, device=dev) for name, (n, dtype) in sizes.items()}
-            if count:
-                # the zeros are written on torch's stream, the steps run on the context's
-                torch.cuda.current_stream().synchronize()
-        elif count:
+        if state is not None and self.params:
             _on_current_device(**state)
-        self._owns_state = own_state and count > 0
-        self.state = dict(state)
-        everything = self.params + given + list(self.state.values())
-        begins, ends = list(map(torch.Tensor.data_ptr, everything)), []
-        for begin, t in zip(begins, everything):
-            ends.append(begin + t.nbytes)
-        spans = sorted(x for x in zip(begins, ends) if x[1] > x[0])
+
+    def _where(self):
+        """What tells that a tensor is another one or has other memory than at the last step
+        (the copies' places in the list, as some may be None)."""
+        copies = [c for c in self.copies if c is not None]
+        return list(map(torch.Tensor.data_ptr, self.params + copies + list(self.state.values()))), list(
+            map(_NBYTES, self.params)), list(map(id, self.copies))
+
+    def _bind(self):
+        """Write the addresses that a step passes on; raise if tensors overlap."""
+        bound = self.params + [c for c in self.copies if c is not None] + list(self.state.values())
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes) for t in bound if t.numel())
         if any(x[1] > y[0] for x, y in zip(spans, spans[1:])):
             raise ValueError("parameters, copies and moments must not overlap")
-        self.starts = self._starts(self.params)[0]
-        self._tensors = (_AdamWTensor * count)()
-        # the tensors' fields, as 64-bit words
-        words = memoryview(self._tensors).cast("B").cast("Q") if count else memoryview(array.array("Q"))
-        stride = ctypes.sizeof(_AdamWTensor) // 8
-
-        def field(name):
-            return words[getattr(_AdamWTensor, name).offset // 8::stride]
-
-        def fill(name, values, typecode="Q"):
-            field(name)[:] = memoryview(array.array(typecode, values)).cast("B").cast("Q")
-
-        fill("param", begins[:count])
-        fill("numel", map(torch.Tensor.numel, self.params))
-        fill("weight_decay", decay, "d")
-        if given:
-            fill("copy", [0 if c is None else c.data_ptr() for c in self.copies])
+        self._fill("param", map(torch.Tensor.data_ptr, self.params))
+        self._fill("copy", [0 if c is None else c.data_ptr() for c in self.copies])
         for name, t in self.state.items():
             per = self.BLOCK if name.endswith("_scales") else 1
             base, size = t.data_ptr(), t.element_size()
-            fill(name, [base + at // per * size for at in self.starts])
-        self._grad_words = field("grad")
-        self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
-                                      moments=MOMENTS[moments])
+            self._fill(name, [base + at // per * size for at in self.starts])
+        # moments made here that others have taken the place of: steps that use them may still run
+        for t in self._own:
+            if self.ctx._h and not any(t is x for x in self.state.values()):
+                t.record_stream(self._stream())
+        self._own = [t for t in self._own if any(t is x for x in self.state.values())]
+        self._bound, self._last_copies = self._where(), list(self.copies)   # (which keeps the ids from being used anew)
+
+    def _follow(self):
+        """Bind anew if a tensor is another one or has other memory than at the last step."""
+        if self._where() != self._bound or not all(map(torch.Tensor.is_contiguous, self.params)):
+            self._check_tensors(self.state)
+            self._bind()
+
+    def _stream(self):
+        return torch.cuda.ExternalStream(self.ctx._stream)
 
     @classmethod
     def _starts(cls, params):
@@ -793,24 +837,19 @@ class AdamW:
             raise ValueError("grads must have one entry per parameter")
         shapes = list(map(_SHAPE, grads))
         if shapes != self._shapes:
+            if len(shapes) != len(self._shapes):
+                raise ValueError("params and copies must keep their lengths")
             got, want = next((g, p) for g, p in zip(shapes, self._shapes) if g != p)
             raise ValueError(f"a gradient must have shape {tuple(want)}, not {tuple(got)}")
-        o = self._options
-        scalars = {}
-        for name, x, dtype in (("lr", lr, torch.float32), ("step", step, torch.int64),
-                               ("grad_scale", grad_scale, torch.float32)):
-            if isinstance(x, torch.Tensor):
-                if x.dtype != dtype or x.numel() != 1:
-                    raise TypeError(f"{name} must be one {dtype} element")
-                scalars[name] = x
-        _on_current_device(**scalars)
         if grad_scale is not None and not isinstance(grad_scale, torch.Tensor):
             raise TypeError("grad_scale must be a tensor")
-        on_device = isinstance(step, torch.Tensor)
+        o = self._options
+        o.lr_dev, o.step_dev = _scalar(lr, torch.float32, "lr"), _scalar(step, torch.int64, "step")
+        o.grad_scale = _scalar(grad_scale, torch.float32, "grad_scale")
+        on_device = o.step_dev is not None
         number = 0 if on_device else self.steps + 1 if step is None else int(step)
-        o.lr, o.lr_dev = (0.0, lr.data_ptr()) if isinstance(lr, torch.Tensor) else (lr, None)
-        o.step, o.step_dev = number, step.data_ptr() if on_device else None
-        o.grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
+        o.lr, o.step = 0.0 if o.lr_dev is not None else lr, number
+        self._follow()
         if grads:
             o.grad_dtype, ptrs = _gradient_list(grads)
             self._grad_words[:] = memoryview(ptrs)
@@ -820,10 +859,10 @@ class AdamW:
 
     def close(self):
         """Wait for the context's stream, if the moments are this object's own, and let go of them."""
-        if self._owns_state and self.ctx._h:
-            torch.cuda.ExternalStream(self.ctx._stream).synchronize()
-        self._owns_state, self.state, self._tensors, self.params = False, {}, None, []
-        self._shapes, self._grad_words = None, None
+        if self._own and self.ctx._h:
+            self._stream().synchronize()
+        self._own, self._last_copies, self.state, self._tensors, self.params = [], [], {}, None, []
+        self._shapes = self._grad_words = self._words = None
 
     def __del__(self):
         try:
