@@ -800,7 +800,9 @@ class AdamW:
             self._bind()
 
     def _stream(self):
-        return torch.cuda.ExternalStream(self.ctx._stream)
+        # (ExternalStream of 0 is not the null stream but one of torch's pool)
+        handle = self.ctx._stream
+        return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
 
     @classmethod
     def _starts(cls, params):

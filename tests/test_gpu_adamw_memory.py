@@ -98,3 +98,28 @@ def test_moments_made_by_the_object_are_kept_until_their_step_is_done(ctx):
     np.testing.assert_allclose(p.cpu().numpy(), 0.5, rtol=1e-6)       # the first step moves by lr
     opt.close()
     other.close()
+
+
+@pytest.mark.parametrize("null", [True, False])
+def test_close_waits_for_the_step(null):
+    """Also where the context works on the null stream, behind work that takes some milliseconds."""
+    s = torch.cuda.default_stream() if null else torch.cuda.Stream()
+    p, g = torch.ones(300, device=DEV), torch.ones(300, device=DEV)
+    a = torch.randn(8192, 8192, device=DEV)
+    done = torch.cuda.Event()
+    torch.cuda.synchronize()
+    c = gift.Context(stream=s.cuda_stream)
+    assert (c._stream == 0) == null
+    opt = gift.AdamW(c, [p])
+    with torch.cuda.stream(s):
+        a @ a                        # (the library's first product loads its code)
+        s.synchronize()
+        for _ in range(20):
+            a @ a
+        opt.step([g], lr=0.5)
+        done.record(s)
+    opt.close()
+    assert done.query()
+    torch.cuda.synchronize()
+    np.testing.assert_allclose(p.cpu().numpy(), 0.5, rtol=1e-6)
+    c.close()
