@@ -450,7 +450,8 @@ gift_status gift_embedding_grad(gift_ctx *ctx, const void *tokens, gift_index_ty
                                 void *scratch, uint64_t scratch_bytes);
 
 /* Scratch bytes of gift_embedding_grad; 0 for T <= 0 and for sizes that it
- * refuses. */
+ * refuses whether it writes or adds.  (Sizes at which it only adds, a written
+ * gradient being more work than one launch takes, have their bytes.) */
 uint64_t gift_embedding_grad_scratch(int32_t N, int64_t T, int64_t V, int64_t d);
 
 /* Scratch bytes of gift_grad_norm. */

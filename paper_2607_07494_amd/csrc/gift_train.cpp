@@ -116,6 +116,13 @@ gift_status gift_embedding(gift_ctx *ctx, const void *table, gift_dtype table_dt
 
 uint64_t gift_embedding_grad_scratch(int32_t N, int64_t T, int64_t V, int64_t d) {
   if (N < 1 || N > 65535 || T <= 0 || T > kMaxIds / N || V < 1 || V > kMaxVocab || d < 1 || d > kMaxWidth) return 0;
+  EmbGradJob j;
+  j.N = N;
+  j.T = T;
+  j.V = V;
+  j.d = d;
+  j.accumulate = true;    // (the form with fewer workgroups)
+  if (embgrad_blocks(j) > kMaxBlocks) return 0;
   return embgrad_scratch(N, T, V, d);
 }
 
