@@ -602,9 +602,14 @@ def embedding(ctx: Context, table, tokens, out, scale: float = 1.0):
                               out.data_ptr(), od))
 
 
+def _int32(n):
+    """n, or the largest int32 in place of a larger number (ctypes takes it modulo 2^32); the library refuses it."""
+    return min(n, 2 ** 31 - 1)
+
+
 def embedding_grad_scratch(N: int, T: int, V: int, d: int) -> int:
     """Scratch bytes of :func:`embedding_grad` (``gift_embedding_grad_scratch``)."""
-    return LIB.gift_embedding_grad_scratch(N, T, V, d)
+    return LIB.gift_embedding_grad_scratch(_int32(N), T, V, d)
 
 
 def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumulate: bool = False, scratch=None):
@@ -622,7 +627,7 @@ def embedding_grad(ctx: Context, tokens, dout, grads, scale: float = 1.0, accumu
         raise TypeError(f"grads must have dtype torch.float32, not {grads.dtype}")
     _on_current_device(tokens=tokens, dout=dout, grads=grads)
     ws, ws_bytes = _scratch(scratch)
-    _check(LIB.gift_embedding_grad(ctx._h, tokens.data_ptr(), it, dout.data_ptr(), dt, N, T, V, d, scale,
+    _check(LIB.gift_embedding_grad(ctx._h, tokens.data_ptr(), it, dout.data_ptr(), dt, _int32(N), T, V, d, scale,
                                    1 if accumulate else 0, grads.data_ptr(), ws, ws_bytes))
 
 

@@ -4,6 +4,7 @@ them, all on the host (no GPU needed): fake pointers are never dereferenced."""
 import ctypes
 
 import pytest
+import torch
 
 gift = pytest.importorskip("paper_2607_07494_amd.gift")
 FAKE = ctypes.c_void_p(0x1000)
@@ -34,3 +35,26 @@ def test_scratch_is_0_where_both_forms_are_refused(N, T, V, d, writes, adds):
         assert (st != gift.ESHAPE) == taken, text
         assert st != gift.OK and (taken or "more work" in text)
     assert (gift.embedding_grad_scratch(N, T, V, d) > 0) == (writes or adds)
+
+
+def test_a_number_of_ranks_past_32_bits_is_not_taken_modulo(monkeypatch):
+    seen = []
+
+    class Library:
+        def gift_embedding_grad(self, *args):
+            seen.append(args[5])
+            return gift.OK
+
+    N = (1 << 32) + 1
+    assert gift.embedding_grad_scratch(N, 4, 4, 4) == 0
+    monkeypatch.setattr(gift, "LIB", Library())
+    monkeypatch.setattr(gift, "_on_current_device", lambda **tensors: None)
+
+    class Context:
+        _h = None
+
+    def meta(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    gift.embedding_grad(Context(), meta(N, 1, dtype=torch.int32), meta(N, 1, 2), meta(N, 3, 2))
+    assert ctypes.c_int32(seen[0]).value > 65535       # refused by the library
