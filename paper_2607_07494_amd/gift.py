@@ -700,8 +700,8 @@ class AdamW:
     ``params``, ``copies`` and ``state`` may change between steps: a step works on the
     tensors that they hold, where those lie, at the time of the call (after
     ``param.data = other`` or ``state["m"] = loaded`` on the other memory).  Shapes
-    and dtypes must stay.  A captured step keeps the addresses
-    that it was captured with.
+    and dtypes must stay.  A captured step keeps the addresses that it was
+    captured with.
     """
 
     ALIGN, BLOCK = 512, 256
@@ -719,15 +719,15 @@ class AdamW:
         if len(decay) != count or len(self.copies) != count:
             raise ValueError("weight_decay and copies must have one entry per parameter")
         self._shapes = list(map(_SHAPE, self.params))
-        self.starts = self._starts(self.params)[0]
+        self.starts, total = self._starts(self.params)
+        self._sizes = self._state_of(total, moments)
         self._tensors = (_AdamWTensor * count)()
         # the tensors' fields, as 64-bit words
         self._words = memoryview(self._tensors).cast("B").cast("Q") if count else memoryview(array.array("Q"))
         self._check_tensors(state)
         if state is None:
             dev = torch.device("cuda", torch.cuda.current_device()) if count else torch.device("cpu")
-            state = {name: torch.zeros(n, dtype=dtype, device=dev)
-                     for name, (n, dtype) in self.state_sizes(self.params, moments).items()}
+            state = {name: torch.zeros(n, dtype=dtype, device=dev) for name, (n, dtype) in self._sizes.items()}
             if count:
                 # the zeros are written on torch's stream, the steps run on the context's
                 torch.cuda.current_stream().synchronize()
@@ -754,16 +754,15 @@ class AdamW:
                 raise TypeError(f"{name} must be {str(dtype)[6:]}, not {set(map(_DTYPE, tensors)) - {dtype}}")
         if len(self.params) != len(self._shapes) or len(self.copies) != len(self._shapes):
             raise ValueError("params and copies must keep their lengths")
-        for shape, p, c in zip(self._shapes, self.params, self.copies):
-            if p.shape != shape:
-                _expect(p, shape, "a parameter")
-            if c is not None and c.shape != shape:
-                _expect(c, shape, "a copy")
+        places = [shape for shape, c in zip(self._shapes, self.copies) if c is not None]
+        for name, tensors, shapes in (("a parameter", self.params, self._shapes), ("a copy", given, places)):
+            if list(map(_SHAPE, tensors)) != shapes:
+                for t, shape in zip(tensors, shapes):
+                    _expect(t, shape, name)
         if state is not None:
-            sizes = self.state_sizes(self.params, self.moments)
-            if set(state) != set(sizes):
-                raise ValueError(f"state must hold {sorted(sizes)}, not {sorted(state)}")
-            for name, (n, dtype) in sizes.items():
+            if set(state) != set(self._sizes):
+                raise ValueError(f"state must hold {sorted(self._sizes)}, not {sorted(state)}")
+            for name, (n, dtype) in self._sizes.items():
                 _expect(state[name], (n,), f"state[{name!r}]")
                 if state[name].dtype != dtype:
                     raise TypeError(f"state[{name!r}] must have dtype {dtype}, not {state[name].dtype}")
@@ -781,12 +780,16 @@ class AdamW:
 
     def _bind(self):
         """Write the addresses that a step passes on; raise if tensors overlap."""
-        bound = self.params + [c for c in self.copies if c is not None] + list(self.state.values())
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes) for t in bound if t.numel())
+        where = self._where()
+        begins, count = where[0], len(self.params)
+        given = [c for c in self.copies if c is not None]
+        sizes = where[1] + list(map(_NBYTES, given)) + list(map(_NBYTES, self.state.values()))
+        spans = sorted((at, at + size) for at, size in zip(begins, sizes) if size)
         if any(x[1] > y[0] for x, y in zip(spans, spans[1:])):
             raise ValueError("parameters, copies and moments must not overlap")
-        self._fill("param", map(torch.Tensor.data_ptr, self.params))
-        self._fill("copy", [0 if c is None else c.data_ptr() for c in self.copies])
+        self._fill("param", begins[:count])
+        places = iter(begins[count:])
+        self._fill("copy", [0 if c is None else next(places) for c in self.copies])
         for name, t in self.state.items():
             per = self.BLOCK if name.endswith("_scales") else 1
             base, size = t.data_ptr(), t.element_size()
@@ -796,7 +799,7 @@ class AdamW:
             if self.ctx._h and not any(t is x for x in self.state.values()):
                 t.record_stream(self._stream())
         self._own = [t for t in self._own if any(t is x for x in self.state.values())]
-        self._bound, self._last_copies = self._where(), list(self.copies)   # (which keeps the ids from being used anew)
+        self._bound, self._last_copies = where, list(self.copies)   # (which keeps the ids from being used anew)
 
     def _follow(self):
         """Bind anew if a tensor is another one or has other memory than at the last step."""
@@ -820,7 +823,10 @@ class AdamW:
     @classmethod
     def state_sizes(cls, params, moments: str = "f32"):
         """``{name: (elements, dtype)}`` of the flat state tensors."""
-        total = cls._starts(params)[1]
+        return cls._state_of(cls._starts(params)[1], moments)
+
+    @classmethod
+    def _state_of(cls, total, moments):
         if moments == "f32":
             return {"m": (total, torch.float32), "v": (total, torch.float32)}
         return {"m": (total, torch.uint8), "v": (total, torch.uint8),
