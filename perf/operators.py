@@ -317,20 +317,24 @@ def _plain_adamw(s):
 # One pass
 # ---------------------------------------------------------------------------
 
-_kept = {}
+_contexts = {}
 
 
-def _context():
-    """The program's context, on the stream that it works on."""
-    if "context" not in _kept:
+def _context(s):
+    """The program's context on the stream of the state's first pass."""
+    if "context" not in s:
         import paper_2607_07494_amd as gift
-        _kept["context"] = gift.Context()
-    return _kept["context"]
+        stream = torch.cuda.current_stream()
+        key = (stream.device_index, stream.cuda_stream)
+        if key not in _contexts:
+            _contexts[key] = gift.Context()
+        s["context"] = _contexts[key]
+    return s["context"]
 
 
 def _own_pass(s):
     import paper_2607_07494_amd as gift
-    ctx, case, kind = _context(), s["case"], s["case"]["kind"]
+    ctx, case, kind = _context(s), s["case"], s["case"]["kind"]
     if kind == "lookup":
         gift.embedding(ctx, s["table"], s["tokens"], s["out"], scale=_scale(case))
         return s["out"]
