@@ -700,8 +700,8 @@ class AdamW:
     ``params``, ``copies`` and ``state`` may change between steps: a step works on the
     tensors that they hold, where those lie, at the time of the call (after
     ``param.data = other`` or ``state["m"] = loaded`` on the other memory).  Shapes
-    and dtypes must stay.  A captured step keeps the addresses that it was
-    captured with.
+    and dtypes must stay.  ``betas``, ``eps`` and ``seed`` may be set between steps too.
+    A captured step keeps what it was captured with.
     """
 
     ALIGN, BLOCK = 512, 256
@@ -710,8 +710,9 @@ class AdamW:
                  moments: str = "f32", seed: int = 0, state=None, copies=None):
         if moments not in MOMENTS:
             raise ValueError(f"moments must be one of {sorted(MOMENTS)}, not {moments!r}")
-        self.ctx, self.params, self.betas, self.eps, self.moments = ctx, list(params), betas, eps, moments
-        self.seed, self.steps = seed, 0
+        self._options = _AdamWOptions(moments=MOMENTS[moments])
+        self._moments, self.betas, self.eps, self.seed = moments, betas, eps, seed
+        self.ctx, self.params, self.steps = ctx, list(params), 0
         self._own = []          # moments made here
         count = len(self.params)
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
@@ -737,8 +738,34 @@ class AdamW:
         self._fill("weight_decay", decay, "d")
         self._bind()
         self._grad_words = self._field("grad")
-        self._options = _AdamWOptions(beta1=betas[0], beta2=betas[1], eps=eps, seed=seed & (2 ** 64 - 1),
-                                      moments=MOMENTS[moments])
+
+    @property
+    def moments(self):
+        return self._moments
+
+    @property
+    def betas(self):
+        return self._options.beta1, self._options.beta2
+
+    @betas.setter
+    def betas(self, betas):
+        self._options.beta1, self._options.beta2 = betas
+
+    @property
+    def eps(self):
+        return self._options.eps
+
+    @eps.setter
+    def eps(self, eps):
+        self._options.eps = eps
+
+    @property
+    def seed(self):
+        return self._options.seed
+
+    @seed.setter
+    def seed(self, seed):
+        self._options.seed = seed & (2 ** 64 - 1)
 
     def _field(self, name):
         return self._words[getattr(_AdamWTensor, name).offset // 8::ctypes.sizeof(_AdamWTensor) // 8]

@@ -11,6 +11,8 @@ class Library:
     """``gift_adamw_step`` that keeps the tensors' fields of its last call."""
 
     def gift_adamw_step(self, ctx, count, tensors, options):
+        o = options._obj
+        self.options = (o.beta1, o.beta2, o.eps, o.seed, o.moments)
         self.tensors = [{f: getattr(tensors[i], f) for f, _ in gift._AdamWTensor._fields_} for i in range(count)]
         return gift.OK
 
@@ -153,3 +155,15 @@ def test_lists_of_another_length_are_refused(lib, ctx):
     opt.params.append(torch.zeros(5))
     with pytest.raises(ValueError, match="keep their lengths"):
         opt.step(gradients(opt), lr=0.1)
+
+
+def test_betas_eps_and_seed_set_between_steps_reach_the_library(lib, ctx):
+    opt = optimizer(ctx, "e4m3")
+    opt.step(gradients(opt), lr=0.1)
+    assert lib.options == (0.9, 0.95, 1e-8, 0, 1)
+    opt.betas, opt.eps, opt.seed = (0.8, 0.99), 1e-6, -1
+    assert (opt.betas, opt.eps, opt.seed) == ((0.8, 0.99), 1e-6, 2 ** 64 - 1)
+    opt.step(gradients(opt), lr=0.1)
+    assert lib.options == (0.8, 0.99, 1e-6, 2 ** 64 - 1, 1)
+    with pytest.raises(AttributeError):
+        opt.moments = "f32"
