@@ -106,12 +106,7 @@ __device__ __forceinline__ void store_row(float *p, const float v[VEC]) {
 
 template <int VEC>
 __device__ __forceinline__ void store_row(uint16_t *p, const float v[VEC]) {
-  if constexpr (VEC == 8) {
-    uintx4_u x;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = to_bf16(v[2 * k]) | to_bf16(v[2 * k + 1]) << 16;
-    *reinterpret_cast<uintx4_u *>(p) = x;
-  } else if constexpr (VEC == 4) {
+  if constexpr (VEC == 4) {
     uintx2_u x;
 #pragma unroll
     for (int k = 0; k < 2; ++k) x[k] = to_bf16(v[2 * k]) | to_bf16(v[2 * k + 1]) << 16;
@@ -180,7 +175,7 @@ constexpr int lookup_rows() {
   return VEC * sizeof(TIn) >= 32 ? 2 : 4;
 }
 
-template <typename TIn, typename TOut, int VEC, bool STREAM>
+template <typename TIn, typename TOut, int VEC>
 __global__ __launch_bounds__(256) void lookup_kernel(const TIn *table, const void *tokens, bool wide, int64_t T,
                                                      int64_t V, int64_t d, int chunks, float scale, TOut *out) {
   constexpr int kLookupRows = lookup_rows<TIn, VEC>();
@@ -204,9 +199,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const TIn *table, const voi
 #pragma unroll
       for (int k = 0; k < VEC; ++k) v[k] = in[r] ? x[r][k] * scale : 0.f;
       // (a row's last lane rewrites columns of the one before with the same values)
-      TOut *p = out + (t0 + r) * d + c.first;
-      if constexpr (STREAM) stream_row<VEC>(p, v);
-      else store_row<VEC>(p, v);
+      stream_row<VEC>(out + (t0 + r) * d + c.first, v);
     }
   }
 }
@@ -853,34 +846,33 @@ GradPlan grad_plan(int64_t N, int64_t T, int64_t V, int64_t d) {
   return p;
 }
 
-template <typename TIn, typename TOut, int VEC, bool STREAM>
+template <typename TIn, typename TOut, int VEC>
 void lookup_launch(gift_ctx *ctx, const LookupJob &j) {
   constexpr int rows = lookup_rows<TIn, VEC>();
   const int chunks = (int)column_chunks(j.d, VEC);
   const int64_t waves = (j.T + rows - 1) / rows * chunks;
-  hipLaunchKernelGGL((lookup_kernel<TIn, TOut, VEC, STREAM>), dim3(blocks_for(waves < 65536 * 4 ? waves : 65536 * 4)),
+  hipLaunchKernelGGL((lookup_kernel<TIn, TOut, VEC>), dim3(blocks_for(waves < 65536 * 4 ? waves : 65536 * 4)),
                      dim3(256), 0, ctx->stream, static_cast<const TIn *>(j.table), j.tokens, j.wide, j.T, j.V, j.d,
                      chunks, j.scale, static_cast<TOut *>(j.out));
 }
 
 // A float32 row is stored 16 bytes a lane, so that an instruction writes one
-// span, and where rows do not start on 16 bytes the caches join their ends
-// (65536 x 771: streamed 63 us, else 50; bfloat16 rows 26 either way).
+// span; past the caches wherever rows start (65536 x 771 from a float32 table:
+// through them 73 us, past them 52; x 259 from bfloat16 30 and 17).
 template <typename TIn>
 void lookup_launch(gift_ctx *ctx, const LookupJob &j) {
   const int vec = lane_columns(j.d);
   if (j.out_bf16) {
-    if (vec == 8) lookup_launch<TIn, uint16_t, 8, true>(ctx, j);
-    else if (vec == 4) lookup_launch<TIn, uint16_t, 4, true>(ctx, j);
-    else if (vec == 2) lookup_launch<TIn, uint16_t, 2, true>(ctx, j);
-    else lookup_launch<TIn, uint16_t, 1, true>(ctx, j);
+    if (vec == 8) lookup_launch<TIn, uint16_t, 8>(ctx, j);
+    else if (vec == 4) lookup_launch<TIn, uint16_t, 4>(ctx, j);
+    else if (vec == 2) lookup_launch<TIn, uint16_t, 2>(ctx, j);
+    else lookup_launch<TIn, uint16_t, 1>(ctx, j);
   } else if (vec >= 4) {
-    if (j.d % 4 == 0 && (reinterpret_cast<uintptr_t>(j.out) & 15) == 0) lookup_launch<TIn, float, 4, true>(ctx, j);
-    else lookup_launch<TIn, float, 4, false>(ctx, j);
+    lookup_launch<TIn, float, 4>(ctx, j);
   } else if (vec == 2) {
-    lookup_launch<TIn, float, 2, true>(ctx, j);
+    lookup_launch<TIn, float, 2>(ctx, j);
   } else {
-    lookup_launch<TIn, float, 1, true>(ctx, j);
+    lookup_launch<TIn, float, 1>(ctx, j);
   }
 }
 
