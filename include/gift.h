@@ -62,6 +62,8 @@
 extern "C" {
 #endif
 
+/* Raised when a declaration changes; new functions, new enum values and a larger
+ * GIFT_KERNEL_COUNT leave it (a library that lacks them lacks the symbols). */
 #define GIFT_ABI_VERSION 1
 
 typedef struct gift_ctx gift_ctx;
@@ -438,8 +440,9 @@ gift_status gift_embedding(gift_ctx *ctx, const void *table, gift_dtype table_dt
  *           gift_embedding_grad_scratch(N, T, V, d) bytes, scratch_bytes of it.
  * Positions are ordered by token (a stable sort), a row's terms are added in
  * float32 in runs of neighbouring positions, the runs' sums in a fixed order: the same
- * inputs give the same bits.  T may be 0.  Any element alignment of dout and
- * grads.
+ * inputs give the same bits.  The runs' sums of one row are added one after the
+ * other in at most four shares, so rounding and time grow with the most frequent
+ * token's count.  T may be 0.  Any element alignment of dout and grads.
  * Errors: GIFT_EINVAL (NULL, bad type, scale not finite, scratch too small or
  * misaligned), GIFT_ESHAPE (N not in [1, 65535], T < 0, N T >= 2^31, V not in
  * [1, 2^31 - 2], d not in [1, 2^20], or more work than one launch takes),
@@ -459,7 +462,9 @@ uint64_t gift_embedding_grad_scratch(int32_t N, int64_t T, int64_t V, int64_t d)
 
 /* Global norm of many gradients, and the coefficient that clips it:
  *   out[0] = norm = sqrt(sum of all squares);
- *   out[1] = min(1, max_norm / (norm + 1e-6)), NaN when the norm is not finite.
+ *   out[1] = min(1, max_norm / (norm + 1e-6)), NaN when the norm is not finite
+ *            (in float64: finite gradients have a coefficient, also where out[0]
+ *            is past float32's range and infinite).
  *   grads, numel  HOST arrays of count device pointers and element counts
  *                 (an entry of 0 elements is skipped, its pointer may be NULL),
  *                 all float32 or all bfloat16;

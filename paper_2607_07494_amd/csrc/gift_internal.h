@@ -413,6 +413,8 @@ gift_status upload_table(gift_ctx *ctx, int kind, const void *owner, const void 
 // ---------------------------------------------------------------------------
 // The training step around the codec (k_embed.hip, k_optim.hip)
 // ---------------------------------------------------------------------------
+inline bool aligned(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
 struct LookupJob {
   const void *table = nullptr, *tokens = nullptr;
   void *out = nullptr;

@@ -16,8 +16,6 @@ constexpr int64_t kMaxVocab = (1LL << 31) - 2;
 constexpr int64_t kMaxWidth = 1LL << 20;
 constexpr int64_t kMaxElements = 1LL << 33;      // of a tensor: one launch takes its chunks
 
-bool aligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
 bool is_dtype(int t) { return t == GIFT_F32 || t == GIFT_BF16; }
 
 gift_status fail(gift_status st, const char *call, const char *what) {

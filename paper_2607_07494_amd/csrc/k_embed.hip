@@ -6,16 +6,18 @@
 //
 // The gradient first orders each rank's positions by token (stable radix sort),
 // so that a row's terms are neighbours and stand in position order.  The
-// ordered list is cut into runs of 8 to 32 entries, one wave each: the work
-// does not depend on how often a token occurs.  A wave adds its entries' rows
-// in float32 and stores every row that begins and ends in its run; the parts of
-// rows that cross a border go to scratch and a second kernel adds them in a
-// fixed order.  No atomics on values: the same inputs give the same bits.  Rows
-// without a token are zeroed by further workgroups of the same launch.
+// ordered list is cut into runs of 8 to 32 entries, one wave each, whatever
+// tokens they are of.  A wave adds its entries' rows in float32 and stores every
+// row that begins and ends in its run; the parts of rows that cross a border go
+// to scratch and a second kernel adds them in a fixed order, all parts of a row
+// in one workgroup a column chunk: its time grows with the most frequent
+// token's count.  No atomics on values: the same inputs give the same bits.
+// Rows without a token are zeroed by further workgroups of the same launch.
 //
 // Ids outside [0, V) (padding) get the sort key V, the largest: they end up
 // behind all others and nothing reads them.
 
+#include "bf16.h"
 #include "gift_internal.h"
 #include "xcd_map.h"
 
@@ -29,15 +31,6 @@ typedef float floatx4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t uintx4_u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t uintx2_u __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t uintx1_u __attribute__((aligned(2)));
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// float32 -> bfloat16, to nearest even; a NaN stays one
-__device__ __forceinline__ uint32_t to_bf16(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return x != x ? (u >> 16 | 0x40u) : (u + 0x7fffu + (u >> 16 & 1u)) >> 16;
-}
 
 template <bool STREAM, typename W>
 __device__ __forceinline__ W fetch(const W *p) {
@@ -530,7 +523,7 @@ struct SumArgs {
   int64_t runs, chunks, run_waves;
   int64_t zero_groups, zero_ranks;   // groups of zero_rows table rows of a rank; ranks to look over
   int64_t run_blocks;                // workgroups of the runs, a multiple of 8; one a zero group follows
-  int run;                           // ordered entries of one wave, at most 64
+  int run;                           // ordered entries of one wave, 8 to 32
   int zero_rows;                     // table rows looked over by one workgroup, a power of two up to 32
   float scale;
 };
@@ -676,6 +669,9 @@ __global__ __launch_bounds__(256) void embgrad_sum_kernel(SumArgs a) {
 // parts it adds itself, in order, longer rows are left to the whole workgroup,
 // a share of the parts a wave and then the shares' sums in order.  (A workgroup
 // for each run spent most of its 13 us at 65536 x 1536 on being launched.)
+// A row's parts are looked up 64 runs at a time and added eight at a time, one
+// after the other: 65536 bfloat16 rows of 1536, tokens by Zipf's law, every other
+// one the same, all the same: 101, 118, 144 us written and 97, 110, 114 added.
 constexpr int kJoinAlone = 8, kJoinWaves = 4;
 
 template <int VEC>
@@ -787,8 +783,8 @@ unsigned blocks_for(int64_t waves) { return (unsigned)((waves + 3) / 4); }
 // loads of bfloat16 on wide ones.
 int lane_columns(int64_t d) { return d > 256 ? 8 : d > 128 ? 4 : d > 64 ? 2 : 1; }
 
-// A sum takes at most four: 65536 float32 rows of 1536 in 164 us (eight: 180);
-// an accumulating one holds the old rows too.
+// A sum takes at most four: 65536 rows of 1536 written, float32 136 us (eight:
+// 161), bfloat16 101 (111); added 129 (146) and 97 (102).
 int sum_columns(int64_t d) {
   const int vec = lane_columns(d);
   return vec > 4 ? 4 : vec;
@@ -806,7 +802,8 @@ int run_length(int64_t N, int64_t T, int64_t d) {
   return run;
 }
 
-// Table rows that a workgroup looks over for empty ones: about 16 KB.
+// Table rows that a workgroup looks over for empty ones: 16 to 32 KB of widths
+// from 128 to 1024; 32 narrower rows, four wider ones.
 int zero_rows_of(int64_t d) {
   int rows = 4;
   while (rows < 32 && rows * d < 4096) rows *= 2;
@@ -880,8 +877,11 @@ template <typename TIn, int VEC, bool ACC>
 gift_status sum_launch(gift_ctx *ctx, const SumArgs &a) {
   // How fast memory takes the zeros hangs on how much of it is written at the
   // same time: 8 x 32000 x 1024 by waves of 16 KB each 206 us, by workgroups of
-  // 16 KB whose neighbours run on one XCD 193, and with three of them a CU, which
-  // this much LDS makes it, 170.  (The search for empty rows wants more waves.)
+  // 16 KB whose neighbours run on one XCD 197, and with three of them a CU, which
+  // this much LDS makes it, 172.  Sums with few rows to clear do not lose by it:
+  // 8 ranks of 8192 positions with 8000, 4000 and 1000 rows 98, 81 and 65 us
+  // without, 92, 74 and 62 with; one rank with 1000 rows of 1536 31.1 and 30.9.
+  // (The search for empty rows wants more waves.)
   const unsigned lds = a.zero_ranks > 0 && a.present ? 52 * 1024 : 0;
   hipLaunchKernelGGL((embgrad_sum_kernel<TIn, VEC, ACC>),
                      dim3((unsigned)(a.run_blocks + a.zero_ranks * a.zero_groups)), dim3(256), lds, ctx->stream, a);

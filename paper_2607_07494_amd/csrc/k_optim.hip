@@ -7,10 +7,10 @@
 
 #include <math.h>
 
+#include "bf16.h"
 #include "fp8_e4m3.h"
 #include "gift_internal.h"
 #include "philox.h"
-#include "xcd_map.h"
 
 namespace gift {
 
@@ -19,15 +19,6 @@ namespace {
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// float32 -> bfloat16, to nearest even; a NaN stays one
-__device__ __forceinline__ uint32_t to_bf16(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return x != x ? (u >> 16 | 0x40u) : (u + 0x7fffu + (u >> 16 & 1u)) >> 16;
-}
 
 // index of the last of `count` ascending first chunks that is <= chunk
 __device__ __forceinline__ int find_tensor(const uint32_t *first, int count, uint32_t chunk) {
@@ -44,7 +35,9 @@ __device__ __forceinline__ int find_tensor(const uint32_t *first, int count, uin
 // Squares and sums in float64: no overflow of a square, and the result does
 // not depend on how the elements are spread over the workgroups beyond its
 // last bits.  Bound by reading the gradients once: past the caches, 374 M
-// float32 elements in 224 us, 6.7 TB/s (through them 247 us).
+// float32 elements in 224 us, 6.7 TB/s (through them 247 us).  Tensors that do
+// not start on 16 bytes are read element by element: 315 M float32 elements 351
+// instead of 183 us, bfloat16 318 instead of 102.
 constexpr int kNormTensors = 128;
 constexpr int kNormChunk = 4096;      // elements of a workgroup's step
 constexpr int kNormGroups = 2048;     // workgroups, one partial sum each
@@ -174,6 +167,9 @@ __host__ __device__ __forceinline__ void bias_corrections(double lr, int64_t ste
   s.step = (uint32_t)step;
 }
 
+// A learning rate or step of the device's is worked out by every lane, beside
+// the other waves' loads: 315 M elements in a replayed graph 1640 us with float32
+// and 957 with 8-bit moments, by the host's scalars 1675 and 968.
 __device__ __forceinline__ AdamStep adam_step(const AdamArgs &a, const AdamTensor &t, float &keep) {
   AdamStep s = a.host;
   keep = t.keep;
@@ -419,8 +415,6 @@ __global__ __launch_bounds__(256) void adamw_e4m3_kernel(AdamArgs a) {
   }
 }
 
-bool aligned(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
 }  // namespace
 
 size_t grad_norm_scratch() { return kNormGroups * sizeof(double); }
@@ -498,6 +492,8 @@ gift_status launch_adamw(gift_ctx *ctx, int32_t count, const gift_adamw_tensor *
       t.decay = x.weight_decay;
       t.keep = (float)(1.0 - o.lr * x.weight_decay);
       t.index = (uint32_t)i;
+      // else element by element: 315 M elements, each array one off, float32 moments
+      // 1840 us (aligned 1685), 8-bit moments 2015 (970)
       if (aligned(x.param, 16) && aligned(x.grad, bf16 ? 8 : 16) && aligned(x.m, eight ? 4 : 16) &&
           aligned(x.v, eight ? 4 : 16) && aligned(x.copy, 8))
         a.vec |= 1ull << a.count;
